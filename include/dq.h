@@ -262,6 +262,64 @@ int dq_codec_round_host(dq_ctx* ctx, const float* v_host, uint32_t round, float 
 int dq_quantize_pack_static(const float* v, int64_t d, int M, int b, uint64_t seed, uint32_t round,
                             uint8_t* codes, int64_t stride, float* scale, void* stream);
 
+/* ---- losses of a large output layer (a vocabulary) -------------------------------------------------------------
+ * The paper's network ends in softmax cross-entropy over a few classes (Section 5.2; DQ_MODEL_MLP).  These calls are the
+ * same layer for many: logits z = h w^T of n rows of hidden values over V classes, of which no n x V array is kept.
+ * Their gradients are what a worker of such a model hands to the codec (grad_w as the vector v of dq_codec_round).
+ * They need no dq_ctx: the caller owns a workspace and may keep it for any number of calls.
+ *
+ * With T the temperature (1 for cross-entropy), lse_n = log sum_v exp(z_nv / T):
+ *   cross-entropy  loss_n = lse_n - z_n,label
+ *   distillation   entries (top_idx, top_logits) [n][k] of the teacher's largest logits.  An entry is present if its class is
+ *                  in 0..V-1 and its logit is not -inf; q = exp(top_logit / T - tl), where tl is teacher_lse[n], the teacher's
+ *                  own log sum exp(logit / T) over all classes, or, for teacher_lse = NULL, that over the row's present entries.
+ *                  loss_n = T^2 sum_present q (log q - (z_n,idx / T - lse_n));  the mass outside the list adds nothing.
+ *                  A class listed twice counts as two entries.
+ *   gradients      of F = sum_n weight[n] loss_n:  grad_h [n][d], grad_w [V][d].  weight = NULL: 1 / (rows with a target),
+ *                  the mean.
+ * A row without a target (label outside 0..V-1, no present entry) has loss 0, lse 0, a zero row of grad_h and no part in
+ * grad_w, whatever its h holds.  A NaN or Inf elsewhere spreads as the formulas say.  Not in place: outputs may not
+ * overlap inputs or each other.
+ *
+ * Types: h, w and the gradients fp32 (DQ_DENSE_F32) or bfloat16 (DQ_DENSE_BF16); everything else fp32 or int32.  Products
+ * run on the tensor cores with fp32 accumulation: bfloat16 as it is, with dF/dz rounded to bfloat16 before the gradients'
+ * products; fp32 as three bfloat16 terms (24 bits), dF/dz too.  Sums have a fixed order: equal inputs give equal bytes.
+ *
+ * The workspace belongs to one call at a time: calls (or captured graphs) whose GPU work may overlap need one each.  No
+ * call allocates or synchronises (dq_vocab_status does), so all can be captured.  Launches go to the current device, which
+ * must be the one the tensors are on. */
+#define DQ_VOCAB_MAX_TOP 256
+typedef struct {
+    int32_t format;            /* DQ_DENSE_F32 or DQ_DENSE_BF16                                             */
+    int32_t k;                 /* distillation: entries per row, 1..DQ_VOCAB_MAX_TOP; cross-entropy: 0      */
+    int64_t n, d, V;           /* rows 0..2^24, hidden size 1..2^16, classes 1..2^28                        */
+    const void* h; int64_t ld_h;   /* [n][d], ld_h >= d elements from one row to the next, at most 2^32     */
+    const void* w; int64_t ld_w;   /* [V][d].  bfloat16 rows that start on 16 bytes are read in place; others are
+                                      copied into the workspace by every call                               */
+    void* workspace; int64_t workspace_bytes;   /* 256-byte aligned, at least dq_vocab_workspace_bytes      */
+} dq_vocab;
+
+/* Bytes that the calls on these shapes need (grad = 0: the losses alone); -1 for sizes out of range.  Looks at format, k,
+ * n, d, V, w and ld_w only; asks the current device for its number of SMs. */
+int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad);
+
+/* loss [n]; lse [n] or NULL; labels [n]. */
+int dq_xent_loss(const dq_vocab* v, const int32_t* labels, float* loss, float* lse, void* stream);
+
+/* The losses and both gradients.  weight [n] or NULL. */
+int dq_xent_grad(const dq_vocab* v, const int32_t* labels, const float* weight, float* loss, float* lse, void* grad_h, int64_t ld_gh,
+                 void* grad_w, int64_t ld_gw, void* stream);
+
+/* top_idx, top_logits [n][k]; teacher_lse [n] or NULL; temperature > 0. */
+int dq_distill_loss(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,
+                    float* loss, float* lse, void* stream);
+int dq_distill_grad(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,
+                    const float* weight, float* loss, float* lse, void* grad_h, int64_t ld_gh, void* grad_w, int64_t ld_gw, void* stream);
+
+/* Synchronises `stream` and returns the device status of the workspace's last call through *status (HOST): DQ_OK, or
+ * DQ_ERR_TIMEOUT if a wait inside a kernel ran out, which leaves that call's outputs incomplete. */
+int dq_vocab_status(const dq_vocab* v, int* status, void* stream);
+
 /* Test utility: dequantise message w of `msgs` into out [d] (zeros where a sparse message has no entry). */
 int dq_unpack(dq_ctx* ctx, const dq_msgs* msgs, int w, float* out, void* stream);
 

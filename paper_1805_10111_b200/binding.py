@@ -21,7 +21,9 @@ EXPORTS = ["dq_packed_bytes", "dq_create", "dq_destroy", "dq_epoch_begin", "dq_q
            "dq_norm_inf", "dq_quantize_sparsify_pack", "dq_master_unpack_aggregate_prox", "dq_round", "dq_codec_round",
            "dq_codec_host_setup", "dq_codec_round_host", "dq_unpack", "dq_objective", "dq_round_buffers",
            "dq_poll_status", "dq_launch_count", "dq_strerror", "dq_quantize_pack_static", "dq_select_model_bits",
-           "dq_last_model_bits", "dq_rounds", "dq_set_delays"]
+           "dq_last_model_bits", "dq_rounds", "dq_set_delays", "dq_vocab_workspace_bytes", "dq_xent_loss", "dq_xent_grad",
+           "dq_distill_loss", "dq_distill_grad", "dq_vocab_status"]
+DQ_VOCAB_MAX_TOP = 256
 
 
 class dq_data(C.Structure):
@@ -45,6 +47,12 @@ class dq_state(C.Structure):
 class dq_msgs(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("stride", C.c_int64), ("scale", C.c_void_p),
                 ("idx", C.c_void_p), ("cap", C.c_int64), ("nnz", C.c_void_p)]
+
+
+class dq_vocab(C.Structure):
+    _fields_ = [("format", C.c_int32), ("k", C.c_int32), ("n", C.c_int64), ("d", C.c_int64), ("V", C.c_int64),
+                ("h", C.c_void_p), ("ld_h", C.c_int64), ("w", C.c_void_p), ("ld_w", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
 class DqError(RuntimeError):
@@ -89,6 +97,12 @@ def lib():
             "dq_strerror": (C.c_char_p, [i32]),
             "dq_select_model_bits": (i32, [vp, vp, vp, vp, f32, vp, vp, vp]),
             "dq_last_model_bits": (i32, [vp, C.POINTER(C.c_int32), vp]),
+            "dq_vocab_workspace_bytes": (i64, [vp, i32]),
+            "dq_xent_loss": (i32, [vp, vp, vp, vp, vp]),
+            "dq_xent_grad": (i32, [vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]),
+            "dq_distill_loss": (i32, [vp, vp, vp, vp, f32, vp, vp, vp]),
+            "dq_distill_grad": (i32, [vp, vp, vp, vp, f32, vp, vp, vp, vp, i64, vp, i64, vp]),
+            "dq_vocab_status": (i32, [vp, C.POINTER(C.c_int), vp]),
             "dq_quantize_pack_static": (i32, [vp, i64, i32, i32, C.c_uint64, u32, vp, i64, vp, vp]),
         }
         for name, (res, args) in sig.items():
@@ -162,6 +176,59 @@ class Msgs:
         self.idx = torch.zeros((cfg.M, max(self.cap, 1)), dtype=torch.int32, device=device) if sparse else None
         self.nnz = torch.zeros(cfg.M, dtype=torch.int32, device=device) if sparse else None
         self.c = dq_msgs(_ptr(self.codes), self.stride, _ptr(self.scale), _ptr(self.idx), self.cap, _ptr(self.nnz))
+
+
+class Vocab:
+    """Hidden states h [n, d], weights w [V, d] of a large output layer, a workspace for the losses over them (with their
+    gradients unless grad=False) and the dq_vocab view.  Rows may be strided (the last dimension is contiguous).  k: the
+    teacher's entries per row for the distillation calls, 0 for cross-entropy.  `workspace`: a uint8 tensor to use
+    instead of a new one, of at least workspace_bytes(h, w, k, grad) bytes; it serves one call at a time."""
+
+    def __init__(self, h, w, k=0, grad=True, workspace=None):
+        import torch
+        self.h, self.w, self.device = h, w, w.device
+        self.grad = bool(grad)
+        self.c = self._shape(h, w, k)
+        self.n, self.d, self.V, self.k = self.c.n, self.c.d, self.c.V, self.c.k
+        if h.device != w.device:
+            raise DqError(DQ_ERR_ARG, "Vocab: h and w are on different devices")
+        if workspace is None:
+            workspace = torch.empty(self._bytes(self.c, grad, w.device), dtype=torch.uint8, device=w.device)
+        elif workspace.device != w.device or not workspace.is_contiguous():
+            raise DqError(DQ_ERR_ARG, "Vocab: workspace")
+        self.workspace = workspace
+        self.c.workspace, self.c.workspace_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+        self.ref = C.byref(self.c)
+
+    @staticmethod
+    def _shape(h, w, k):
+        import torch
+        formats = {torch.float32: DQ_DENSE_F32, torch.bfloat16: DQ_DENSE_BF16}
+        if h.dtype not in formats or w.dtype != h.dtype:
+            raise DqError(DQ_ERR_ARG, "Vocab: h and w are both float32 or both bfloat16")
+        if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[1]:
+            raise DqError(DQ_ERR_SHAPE, "Vocab: h is [n, d], w is [V, d]")
+        return dq_vocab(formats[h.dtype], int(k), h.shape[0], h.shape[1], w.shape[0], _ptr(h), _pitch(h), _ptr(w), _pitch(w), None, 0)
+
+    @staticmethod
+    def _bytes(c, grad, device):
+        import torch
+        with torch.cuda.device(device):
+            need = int(lib().dq_vocab_workspace_bytes(C.byref(c), int(bool(grad))))
+        if need < 0:
+            raise DqError(DQ_ERR_ARG, "Vocab: sizes out of range")
+        return need
+
+    @staticmethod
+    def workspace_bytes(h, w, k=0, grad=True):
+        return Vocab._bytes(Vocab._shape(h, w, k), grad, w.device)
+
+
+def _pitch(t):
+    """Elements from one row of a 2-d tensor to the next; -1 (refused by the library) if its last dimension is not contiguous."""
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        return -1
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def make_config(d, M, B=1, bx=8, b=8, lambda1=0.0, lambda2=0.0, box_lo=float("-inf"), box_hi=float("inf"), sparsify=0,
@@ -290,6 +357,69 @@ def dq_quantize_pack_static(v, d, M, b, seed, round_, codes, stride, scale, stre
     """Context-free dense quantise + pack that allocates nothing (scratch is a fixed array inside the library)."""
     return lib().dq_quantize_pack_static(_ptr(v), int(d), int(M), int(b), int(seed), int(round_), _ptr(codes), int(stride),
                                          _ptr(scale), _stream(stream))
+
+
+def _bad(layer, tensors, rows, types, sizes):
+    """Whether a tensor of a vocabulary call is not what the library will take it for (None stands for an absent one)."""
+    for t, dt, size in zip(tensors, types, sizes):
+        if t is not None and (str(t.dtype) != dt or t.device != layer.device or not t.is_contiguous() or t.numel() != size):
+            return True
+    for t, like in rows:
+        if t is None or t.dtype != like.dtype or t.device != layer.device or t.shape != like.shape or _pitch(t) < 0:
+            return True
+    return False
+
+
+def _vocab_call(fn, layer, args, stream):
+    import torch
+    if torch.cuda.current_device() == layer.device.index:
+        return fn(layer.ref, *args, _stream(stream))
+    with torch.cuda.device(layer.device):
+        return fn(layer.ref, *args, _stream(stream))
+
+
+_F, _I = "torch.float32", "torch.int32"
+
+
+def dq_vocab_workspace_bytes(layer: Vocab, grad=True):
+    return layer._bytes(layer.c, grad, layer.device)
+
+
+def dq_xent_loss(layer: Vocab, labels, loss, lse=None, stream=None):
+    if _bad(layer, (labels, loss, lse), (), (_I, _F, _F), (layer.n,) * 3):
+        return DQ_ERR_ARG
+    return _vocab_call(lib().dq_xent_loss, layer, (_ptr(labels), _ptr(loss), _ptr(lse)), stream)
+
+
+def dq_xent_grad(layer: Vocab, labels, weight, loss, lse, grad_h, grad_w, stream=None):
+    if _bad(layer, (labels, weight, loss, lse), ((grad_h, layer.h), (grad_w, layer.w)), (_I, _F, _F, _F), (layer.n,) * 4):
+        return DQ_ERR_ARG
+    return _vocab_call(lib().dq_xent_grad, layer, (_ptr(labels), _ptr(weight), _ptr(loss), _ptr(lse), _ptr(grad_h), _pitch(grad_h),
+                                                   _ptr(grad_w), _pitch(grad_w)), stream)
+
+
+def dq_distill_loss(layer: Vocab, top_idx, top_logits, teacher_lse, temperature, loss, lse=None, stream=None):
+    n, k = layer.n, layer.k
+    if _bad(layer, (top_idx, top_logits, teacher_lse, loss, lse), (), (_I, _F, _F, _F, _F), (n * k, n * k, n, n, n)):
+        return DQ_ERR_ARG
+    return _vocab_call(lib().dq_distill_loss, layer, (_ptr(top_idx), _ptr(top_logits), _ptr(teacher_lse), float(temperature), _ptr(loss),
+                                                      _ptr(lse)), stream)
+
+
+def dq_distill_grad(layer: Vocab, top_idx, top_logits, teacher_lse, temperature, weight, loss, lse, grad_h, grad_w, stream=None):
+    n, k = layer.n, layer.k
+    if _bad(layer, (top_idx, top_logits, teacher_lse, weight, loss, lse), ((grad_h, layer.h), (grad_w, layer.w)),
+            (_I, _F, _F, _F, _F, _F), (n * k, n * k, n, n, n, n)):
+        return DQ_ERR_ARG
+    return _vocab_call(lib().dq_distill_grad, layer, (_ptr(top_idx), _ptr(top_logits), _ptr(teacher_lse), float(temperature), _ptr(weight),
+                                                      _ptr(loss), _ptr(lse), _ptr(grad_h), _pitch(grad_h), _ptr(grad_w), _pitch(grad_w)), stream)
+
+
+def dq_vocab_status(layer: Vocab, stream=None):
+    """Returns (status of the call, device status of the workspace's last call)."""
+    s = C.c_int(0)
+    rc = _vocab_call(lambda ref, st: lib().dq_vocab_status(ref, C.byref(s), st), layer, (), stream)
+    return rc, s.value
 
 
 def ok(rc, where=""):

@@ -8,8 +8,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdq.so")
-SOURCES = ["dq_api.cu", "dq_codec.cu", "dq_grad.cu"]
-HEADERS = ["dq_common.cuh", "dq_kernels.cuh"]
+SOURCES = ["dq_api.cu", "dq_codec.cu", "dq_grad.cu", "dq_vocab.cu"]
+HEADERS = ["dq_common.cuh", "dq_kernels.cuh", "dq_mma.cuh"]
 
 
 def _newest_source() -> float:

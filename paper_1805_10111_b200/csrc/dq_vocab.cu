@@ -1,0 +1,915 @@
+// Losses of a large output layer (a vocabulary of V classes) and their gradients: softmax cross-entropy and distillation
+// from a teacher's top logits.  z = h w^T is formed in tiles of tensor memory and never kept.
+//
+// Mathematics.  With c = 1/T (T = 1 for cross-entropy), lse_n = log sum_v exp(c z_nv) and a row's targets (i_k, q_k),
+// S = sum q_k (cross-entropy: one target, q = 1):
+//   loss_n = T^2 sum_k q_k (log q_k - (c z_n,ik - lse_n)),    dF/dz_nv = weight_n T (S_n p_nv - sum_{k: i_k = v} q_k) =: g_nv,
+//   grad_h = g w,   grad_w = g^T h.
+// Plan.  Rows without a target are left out at the start: the others are gathered into a compact copy of h (so padding costs
+// nothing and a NaN in a padded row reaches nothing).  One pass of products leaves (max, sum) per row and 256 columns; a small
+// kernel joins them to lse and the loss.  For the gradient the logits are formed again, a piece of the vocabulary at a time,
+// turned into g (rounded to bf16) in the kernel's epilogue, and two more products read the piece while it is warm.
+// Every sum has a fixed order: equal inputs give equal bytes.
+#include <math.h>
+#include <cuda_bf16.h>
+
+#include "dq_common.cuh"
+#include "dq_mma.cuh"
+
+namespace dq {
+namespace {
+
+using namespace mma;
+
+enum { kLse = 0, kProb = 1, kGradH = 2, kGradW = 3 };     // what a product's epilogue does
+constexpr int kTileN = 256, kTileK = 64;
+constexpr int kMaxTop = DQ_VOCAB_MAX_TOP;
+constexpr int kHalf = kTileN / 2;                         // columns of an epilogue thread
+constexpr int kPiece = 16;                                // columns staged at a time where a row has targets among them
+constexpr int kSegment = 8;                               // tiles of K summed in tensor memory before the sum moves to registers
+constexpr int64_t kGradBytes = 256ll << 20;               // bound on the piece of g kept between products
+
+struct Ctrl { int status; int count; };                   // head of the workspace: sticky status, rows with a target
+
+// The workspace, carved from the caller's buffer (all parts 256-byte aligned).
+struct Work {
+    Ctrl* ctrl;
+    int32_t *map, *inv, *tgt;      // compact row -> row, row -> compact row or -1, distillation: 0 / -1 has a target
+    float4* rowc;                  // compact row: maximum in log2 units, factor of 2^(z - maximum), factor of q
+    int32_t* eidx; float *eq, *elq, *emass;   // distillation: targets of a row by ascending class, q, log q, sum q
+    float* zt;                     // logit at every target
+    __nv_bfloat16* hp;             // [terms][n_pad][dp] compact rows of h
+    __nv_bfloat16* wp;             // [terms][V][dp] w, where it cannot be read in place
+    float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, log2 units
+    __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
+    float* dh;                     // [splits][n_pad][dq] sums of grad_h
+    // sizes
+    int terms; int64_t n_pad, dp, dq, vc; int vtiles, parts, splits, kps; bool direct_w;
+    int64_t bytes;
+};
+
+bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+// CTAs that share a tile whose M axis are the rows: a pair, unless one CTA's 128 rows hold them all.
+int row_pairs(int64_t n) { return n > 128 ? 2 : 1; }
+
+Work carve(const dq_vocab* v, bool grad, int sms)
+{
+    Work w = {};
+    const bool f32 = v->format == DQ_DENSE_F32;
+    w.terms = f32 ? 3 : 1;
+    w.n_pad = up(v->n > 0 ? v->n : 1, 256);
+    w.dp = up(v->d, 8); w.dq = up(v->d, 8);
+    w.vtiles = (int)((v->V + kTileN - 1) / kTileN); w.parts = 2 * w.vtiles;
+    w.direct_w = !f32 && ptr_aligned(v->w, 16) && v->ld_w % 8 == 0;
+    const int k = v->k > 0 ? v->k : 1;
+    int64_t at = 0;
+    char* base = static_cast<char*>(v->workspace);
+    auto take = [&](int64_t bytes) { char* p = base + at; at = up(at + bytes, 256); return p; };
+    w.ctrl = (Ctrl*)take(sizeof(Ctrl));
+    w.map = (int32_t*)take(4 * w.n_pad); w.inv = (int32_t*)take(4 * w.n_pad);
+    w.rowc = (float4*)take(16 * w.n_pad);
+    w.zt = (float*)take(4 * w.n_pad * k);
+    if (v->k > 0) {
+        w.tgt = (int32_t*)take(4 * w.n_pad); w.emass = (float*)take(4 * w.n_pad);
+        w.eidx = (int32_t*)take(4 * w.n_pad * k); w.eq = (float*)take(4 * w.n_pad * k); w.elq = (float*)take(4 * w.n_pad * k);
+    }
+    w.hp = (__nv_bfloat16*)take(2 * w.terms * w.n_pad * w.dp);
+    if (!w.direct_w) w.wp = (__nv_bfloat16*)take(2 * w.terms * v->V * w.dp);
+    w.part = (float2*)take(8 * w.n_pad * w.parts);
+    if (grad) {
+        int64_t vc = kGradBytes / (2 * w.terms * w.n_pad) / kTileN * kTileN;
+        if (vc < 2 * kTileN) vc = 2 * kTileN;
+        if (vc > up(v->V, kTileN)) vc = up(v->V, kTileN);
+        const int64_t pieces = (v->V + vc - 1) / vc;                       // pieces of nearly the same size
+        w.vc = up((v->V + pieces - 1) / pieces, kTileN);
+        w.g = (__nv_bfloat16*)take(2 * w.terms * w.n_pad * w.vc);
+        // few rows: grad_h has fewer tiles than the GPU has SMs, so its sum over the vocabulary is split and joined
+        const int cg = row_pairs(v->n), units = sms / cg;
+        const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + kTileN - 1) / kTileN));
+        const int kit = (int)(w.vc / kTileK);
+        int splits = tiles < 1 || tiles >= units ? 1 : units / tiles;
+        if (splits > kit / 4) splits = kit / 4 > 0 ? kit / 4 : 1;
+        w.kps = (kit + splits - 1) / splits;
+        w.splits = (kit + w.kps - 1) / w.kps;
+        w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
+    }
+    w.bytes = at;
+    return w;
+}
+
+// ---- small kernels ------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));      // relative error 2^-22
+    return r;
+}
+
+// x as a sum of bf16 terms, each the rounded rest of the ones before: three of them hold all 24 bits of an fp32 value
+// (8 + 1 sign bit of the rest, twice).  A value that rounds past the largest bf16 starts from that instead.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(float x, __nv_bfloat16 (&t)[TERMS])
+{
+    t[0] = __float2bfloat16_rn(x);
+    if (TERMS > 1) {
+        if (isinf(__bfloat162float(t[0])) && !isinf(x)) t[0] = __float2bfloat16_rz(x);
+        float r = isfinite(x) ? x - __bfloat162float(t[0]) : 0.0f;
+#pragma unroll
+        for (int i = 1; i < TERMS; ++i) { t[i] = __float2bfloat16_rn(r); r -= __bfloat162float(t[i]); }
+    }
+}
+
+// One row of `d` values to its bf16 terms (pitch dp, zeros behind the row's end); a warp's work.
+template <bool F32>
+__device__ __forceinline__ void copy_row(const void* src, int64_t off, int d, bool vec, __nv_bfloat16* dst, int64_t plane, int dp, int lane)
+{
+    if (!F32) {
+        const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(src) + off;
+        for (int j = lane * 8; j < dp; j += 256) {
+            uint4 q;
+            if (vec && j + 8 <= d) {
+                q = __ldg(reinterpret_cast<const uint4*>(s + j));
+            } else {
+                __nv_bfloat16 e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = j + i < d ? s[j + i] : __float2bfloat16_rn(0.0f);
+                q = *reinterpret_cast<uint4*>(e);
+            }
+            *reinterpret_cast<uint4*>(dst + j) = q;
+        }
+    } else {
+        const float* s = static_cast<const float*>(src) + off;
+        for (int j = lane * 8; j < dp; j += 256) {
+            float x[8];
+            if (vec && j + 8 <= d) {
+                const float4 a = __ldg(reinterpret_cast<const float4*>(s + j)), b = __ldg(reinterpret_cast<const float4*>(s + j + 4));
+                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = j + i < d ? s[j + i] : 0.0f;
+            }
+            __nv_bfloat16 e[3][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __nv_bfloat16 t[3];
+                split_terms<3>(x[i], t);
+                e[0][i] = t[0]; e[1][i] = t[1]; e[2][i] = t[2];
+            }
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(dst + p * plane + j) = *reinterpret_cast<uint4*>(e[p]);
+        }
+    }
+}
+
+// Targets of the distillation loss: a warp takes a row, orders its present entries by class (ties by place in the list; the
+// epilogues walk them in step with the columns) and forms q.  Absent entries (class outside 0..V-1, logit -inf) go to the end
+// with q = 0.  The rank of an entry is the number of entries before it: K^2 comparisons, K <= 256.
+__global__ void __launch_bounds__(128) vocab_targets_kernel(const int32_t* __restrict__ idx, const float* __restrict__ logits,
+                                                            const float* __restrict__ teacher_lse, float inv_t, int64_t n, int k, int64_t V, Work w)
+{
+    pdl_prologue();
+    __shared__ int32_t s_idx[4][kMaxTop];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + warp; row < n; row += (int64_t)gridDim.x * 4) {
+        const int32_t* ri = idx + row * k; const float* rt = logits + row * k;
+        float m = -INFINITY; bool any = false;
+        for (int j = lane; j < k; j += 32) {
+            int32_t i = ri[j]; const float t = rt[j];
+            if (i < 0 || i >= V || t == -INFINITY) i = INT32_MAX;
+            else { any = true; m = fmaxf(m, t * inv_t); }
+            s_idx[warp][j] = i;
+        }
+        __syncwarp();
+        any = __any_sync(0xFFFFFFFFu, any);
+        float tl;
+        if (teacher_lse) {
+            tl = teacher_lse[row];
+        } else {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            float s = 0.0f;
+            for (int j = lane; j < k; j += 32) if (s_idx[warp][j] != INT32_MAX) s += expf(rt[j] * inv_t - m);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            tl = m + logf(s);
+        }
+        float mass = 0.0f;
+        for (int j = lane; j < k; j += 32) {
+            const int32_t i = s_idx[warp][j];
+            int rank = 0;
+            for (int o = 0; o < k; ++o) { const int32_t x = s_idx[warp][o]; rank += x < i || (x == i && o < j); }
+            float lq = 0.0f, q = 0.0f;
+            if (i != INT32_MAX) { lq = rt[j] * inv_t - tl; q = expf(lq); }
+            mass += q;
+            w.eidx[row * k + rank] = i; w.eq[row * k + rank] = q; w.elq[row * k + rank] = lq;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xFFFFFFFFu, mass, o);
+        if (lane == 0) { w.emass[row] = mass; w.tgt[row] = any ? 0 : -1; }
+        __syncwarp();
+    }
+}
+
+// Compact copy of the rows that have a target.  A block owns a range of rows; it counts the targets before its range (the list
+// is small and in L2) instead of waiting for a scan, then copies its own rows warp by warp.  Rows without a target get loss 0
+// and lse 0 here.  The last block writes the count and zeroes h's rows up to a whole tile of K (a zero of g times whatever the
+// buffer held would be NaN).
+template <bool F32>
+__global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restrict__ h, int64_t ld, int d, const int32_t* __restrict__ tgt, int64_t V,
+                                                           int64_t n, int64_t rows_per_block, bool vec, float* loss, float* lse, Work w)
+{
+    pdl_prologue();
+    __shared__ int s_sum[8];
+    __shared__ int s_rows[256];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t r0 = blockIdx.x * rows_per_block, r1 = min(n, r0 + rows_per_block);
+    int before = 0;
+    for (int64_t r = threadIdx.x; r < r0; r += 256) { const int32_t t = tgt[r]; before += t >= 0 && t < V; }
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (lane == 0) s_sum[warp] = before;
+    __syncthreads();
+    before = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) before += s_sum[i];
+    for (int64_t r = r0; r < r1; r += 256) {
+        __syncthreads();
+        const int64_t mine = r + threadIdx.x;
+        bool has = false;
+        if (mine < r1) { const int32_t t = tgt[mine]; has = t >= 0 && t < V; }
+        const uint32_t bal = __ballot_sync(0xFFFFFFFFu, has);
+        if (lane == 0) s_sum[warp] = __popc(bal);
+        __syncthreads();
+        int off = 0, total = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { if (i < warp) off += s_sum[i]; total += s_sum[i]; }
+        off += __popc(bal & ((1u << lane) - 1u));
+        if (mine < r1) {
+            w.inv[mine] = has ? before + off : -1;
+            if (has) { w.map[before + off] = (int32_t)mine; s_rows[off] = threadIdx.x; }
+            else { loss[mine] = 0.0f; if (lse) lse[mine] = 0.0f; }
+        }
+        __syncthreads();
+        for (int i = warp; i < total; i += 8)
+            copy_row<F32>(h, (r + s_rows[i]) * ld, d, vec, w.hp + (int64_t)(before + i) * w.dp, w.n_pad * w.dp, (int)w.dp, lane);
+        before += total;
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        if (threadIdx.x == 0) { w.ctrl->count = before; w.ctrl->status = DQ_OK; }
+        const int end = (before + kTileK - 1) / kTileK * kTileK;
+        for (int i = before + warp; i < end; i += 8)
+            for (int t = 0; t < w.terms; ++t)
+                for (int j = lane * 8; j < w.dp; j += 256)
+                    *reinterpret_cast<uint4*>(w.hp + (int64_t)t * w.n_pad * w.dp + (int64_t)i * w.dp + j) = make_uint4(0, 0, 0, 0);
+    }
+}
+
+// w where tensor maps cannot read it in place (fp32, or rows that do not start on 16 bytes): its bf16 terms, rows padded.
+template <bool F32>
+__global__ void __launch_bounds__(256) vocab_weights_kernel(const void* __restrict__ src, int64_t ld, int d, int64_t V, bool vec, Work w)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x & 31;
+    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < V; r += (int64_t)gridDim.x * 8)
+        copy_row<F32>(src, r * ld, d, vec, w.wp + r * w.dp, V * w.dp, (int)w.dp, lane);
+}
+
+// Joins the (max, sum) pairs of a row's tiles to lse, forms the loss and the two factors of the gradient; a warp per row.
+__global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const int32_t* __restrict__ labels, const float* __restrict__ weight,
+                                                         float temp, float c2, float* __restrict__ loss, float* __restrict__ lse)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x & 31, count = w.ctrl->count;
+    const double back = 1.0 / ((double)temp * (double)c2);
+    for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < count; i += gridDim.x * 8) {
+        const float2* p = w.part + (int64_t)i * w.parts;
+        float m = -INFINITY, s = 0.0f;
+        for (int t = lane; t < w.parts; t += 32) {
+            const float2 q = p[t];
+            const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
+            s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
+            m = nm;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const float qm = __shfl_xor_sync(0xFFFFFFFFu, m, o), qs = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            const float nm = fmaxf(m, qm), use = nm == -INFINITY ? 0.0f : nm;
+            s = s * exp2f(m - use) + qs * exp2f(qm - use);       // symmetric in the two lanes: all lanes end with the same pair
+            m = nm;
+        }
+        // sum exp(c z) = s 2^m.  The epilogue multiplied by fl(log2(e) / T): m goes back through the same factor, in double, so that
+        // the factor's rounding does not reach lse, and the loss is subtracted before it is rounded
+        const double l = (double)m * back + log((double)s);
+        const int64_t row = w.map[i];
+        double sum = 0.0; float mass = 1.0f;
+        if (k == 0) {
+            sum = l - (double)w.zt[row];
+        } else {
+            for (int j = lane; j < k; j += 32) {
+                const float q = w.eq[row * k + j];
+                if (w.eidx[row * k + j] != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)w.zt[row * k + j] / (double)temp - l));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            sum *= (double)temp * (double)temp;
+            mass = w.emass[row];
+        }
+        if (lane == 0) {
+            loss[row] = (float)sum;
+            if (lse) lse[row] = (float)l;
+            // The mean's factor T / count is left to the end: p - q is rounded to bf16 next, and for the entry that matters most,
+            // p - 1 just inside (-1, 0), the rounding is smallest without it (2^-9 at most, 2^-8 with an unlucky factor)
+            const float wt = weight ? weight[row] * temp : 1.0f;
+            w.rowc[i] = make_float4(m, wt * mass / s, wt, 0.0f);
+        }
+    }
+}
+
+// grad_h = the splits' sums, rounded once; rows without a target get zeros.  A warp per row.
+template <bool F32>
+__global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int64_t n, int d, float scale, void* __restrict__ out, int64_t ld)
+{
+    pdl_prologue();
+    const int lane = threadIdx.x & 31;
+    const float alpha = scale != 0.0f ? scale / (float)max(w.ctrl->count, 1) : 1.0f;
+    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < n; r += (int64_t)gridDim.x * 8) {
+        const int i = w.inv[r];
+        for (int j = lane; j < d; j += 32) {
+            float s = 0.0f;
+            if (i >= 0) for (int q = 0; q < w.splits; ++q) s += w.dh[((int64_t)q * w.n_pad + i) * w.dq + j];
+            s *= alpha;
+            if (F32) static_cast<float*>(out)[r * ld + j] = s;
+            else static_cast<__nv_bfloat16*>(out)[r * ld + j] = __float2bfloat16_rn(s);
+        }
+    }
+}
+
+// ---- the products ---------------------------------------------------------------------------------------------------
+
+struct MmaArgs {
+    int cols;                // extent of the tile's N axis: classes of the piece (kLse, kProb) or d
+    int kdim;                // extent of the summed axis (kGradW: the number of rows with a target, read on the device)
+    int mdim;                // kGradW: classes of the piece; else the number of rows with a target, read on the device
+    int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
+    int splits, kps;         // kGradH: pieces of the summed axis, and their length in tiles of K
+    int v0;                  // first class of the piece
+    int k;                   // targets per row (0: one label)
+    float c2;                // log2(e) / T
+    float scale;             // kGradW: not 0: the result times scale / (rows with a target)
+    int first;               // kGradH: first piece of the vocabulary
+    int align;               // kGradW: rows of the output start on 16 bytes (1), 32 (2) or neither (0)
+    const int32_t* eidx;     // targets' classes [n][max(k, 1)], ascending
+    void* out; int64_t ld;   // kGradW
+};
+
+// Products of bf16 terms for fp32 operands, smallest first so that the leading one is rounded least: (2,0) (0,2) (1,1) (1,0)
+// (0,1) (0,0).  What is left out is below 2^-26 of |a||b|.
+__device__ __forceinline__ int term_a(int p) { return (0x001102 >> (4 * p)) & 15; }
+__device__ __forceinline__ int term_b(int p) { return (0x010120 >> (4 * p)) & 15; }
+
+template <int CG> __host__ __device__ constexpr int stage_bytes() { return 128 * 128 + (kTileN / CG) * 128; }
+template <int CG> __host__ __device__ constexpr int stages() { return CG == 1 ? 4 : 6; }
+constexpr int kStagingBytes = 8 * kPiece * 32 * 4;
+template <int CG> __host__ __device__ constexpr int smem_bytes() { return 1024 + stages<CG>() * stage_bytes<CG>() + kStagingBytes + 256; }
+
+struct Tile { int m, n, split, k0, k1; };
+
+// Tiles in groups of 16 along M, M fastest inside a group: the tiles in flight share few operands and L2 serves the rest.
+__device__ __forceinline__ Tile decode(int t, int mt, int nt, int kit, int kps, bool split_k)
+{
+    Tile r;
+    r.split = t / (mt * nt);
+    t -= r.split * (mt * nt);
+    const int group = t / (16 * nt), first = group * 16, size = min(16, mt - first), q = t - group * 16 * nt;
+    r.m = first + q % size; r.n = q / size;
+    r.k0 = split_k ? r.split * kps : 0;
+    r.k1 = split_k ? min(kit, r.k0 + kps) : kit;
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 lo, __nv_bfloat16 hi)
+{
+    return (uint32_t)__bfloat16_as_ushort(lo) | ((uint32_t)__bfloat16_as_ushort(hi) << 16);
+}
+
+// 32 bytes to one 32-byte sector, or as two stores where the row only starts on 16 bytes.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8], bool wide)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     :: "l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// 16 values as bf16 terms, each term to its plane.
+template <int TERMS>
+__device__ __forceinline__ void store_terms(__nv_bfloat16* dst, int64_t plane, const float* f, bool wide)
+{
+    uint32_t e[TERMS][8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        __nv_bfloat16 t[TERMS], u[TERMS];
+        split_terms<TERMS>(f[i], t);
+        split_terms<TERMS>(f[i + 1], u);
+#pragma unroll
+        for (int p = 0; p < TERMS; ++p) e[p][i / 2] = pack2(t[p], u[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < TERMS; ++p) store32(dst + p * plane, e[p], wide);
+}
+
+// One persistent kernel per product.  Warp 0 loads tiles (TMA, 128-byte swizzle), warp 1 issues the matrix instructions, warps
+// 4-11 turn finished accumulators into results while the next products run: tensor memory holds two accumulators of 128 rows by
+// 256 columns.  The tensor cores cut their fp32 sums off toward zero at every step, which over a long K drifts by about
+// K / 16 * 2^-25 of the sum (measured: 1.0e-5 at K = 4096, 6e-5 at 16384); so a sum stays in tensor memory for 512 of K and
+// the epilogue adds these segments in registers, rounded to nearest, while the next one runs (7e-7 at any K, for free).
+// An epilogue thread owns a row's half tile: its maximum and sum need no exchange between threads.
+// CG = 2: two CTAs on neighbouring SMs share a tile of 256 rows.  Each loads its 128 rows and half of the columns' operand; the
+// even one issues for both.
+template <int CG, int KIND, bool F32>
+__global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+                                                           const MmaArgs a, const Work w)
+{
+    extern __shared__ char smem_raw[];
+    constexpr int NS = stages<CG>(), SB = stage_bytes<CG>(), BN = kTileN / CG;
+    constexpr bool A_MN = KIND == kGradW, B_MN = KIND == kGradH || KIND == kGradW;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
+    float* const staging = reinterpret_cast<float*>(tail);
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(tail + kStagingBytes);     // full[NS], empty[NS], tfull[2], tempty[2], drain
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](int s) { return bar0 + 8 * s; };
+    auto empty = [&](int s) { return bar0 + 8 * (NS + s); };
+    auto tfull = [&](int s) { return bar0 + 8 * (2 * NS + s); };
+    auto tempty = [&](int s) { return bar0 + 8 * (2 * NS + 2 + s); };
+    const uint32_t drain = bar0 + 8 * (2 * NS + 4);
+    volatile int* const gave_up = reinterpret_cast<volatile int*>(bars + 2 * NS + 5);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * NS + 6);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(tfull(s), 1); mbar_init(tempty(s), 8 * CG); }
+        mbar_init(drain, 1);
+        *gave_up = 0;
+        mbar_init_fence();
+        tma_prefetch_map(&ma); tma_prefetch_map(&mb);
+    }
+    if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_slot), 512);
+    fence_before_sync();
+    if (CG == 2) cluster_sync(); else __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    pdl_prologue();
+
+    const int count = w.ctrl->count;
+    const int mdim = KIND == kGradW ? a.mdim : count;
+    const int kit = ((KIND == kGradW ? count : a.kdim) + kTileK - 1) / kTileK;
+    const int mt = (mdim + 128 * CG - 1) / (128 * CG), nt = (a.cols + kTileN - 1) / kTileN;
+    const int tiles = mt * nt * (KIND == kGradH ? a.splits : 1);
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0 && elect_one()) {
+            int s = 0; uint32_t ph = 0; bool ok = true; int issued = 0;
+            for (int t = first; t < tiles && ok; t += step) {
+                const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * kTileN + (int)rank * BN;
+                for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
+                    const int za = term_a(p), zb = term_b(p);
+                    for (int kb = q.k0; kb < q.k1; ++kb) {
+                        if (!mbar_wait(empty(s), ph ^ 1u, gave_up)) { ok = false; break; }
+                        const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
+                        if (rank == 0) mbar_expect_tx(full(s), CG * SB);
+                        const int x = kb * kTileK;
+                        if (!A_MN) {
+                            tma_load<CG>(&ma, dst, bar, x, ym, za);
+                        } else {
+                            tma_load<CG>(&ma, dst, bar, ym, x, za);
+                            tma_load<CG>(&ma, dst + 8192, bar, ym + 64, x, za);
+                        }
+                        if (!B_MN) {
+                            tma_load<CG>(&mb, dst + 16384, bar, x, yn, zb);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < BN / 64; ++j) tma_load<CG>(&mb, dst + 16384 + j * 8192, bar, yn + j * 64, x, zb);
+                        }
+                        ++issued;
+                        if (++s == NS) { s = 0; ph ^= 1u; }
+                    }
+                }
+            }
+            if (!ok && rank == 0) {                       // a wait ran out: let the copies in flight land before the block ends
+                int quiet = 0;
+                for (int i = 0; i < NS && i < issued; ++i) {
+                    if (s == 0) { s = NS; ph ^= 1u; }
+                    --s;
+                    mbar_wait(full(s), ph, &quiet);
+                }
+            }
+        } else if (warp == 1 && rank == 0 && elect_one()) {
+            constexpr uint32_t idesc = instr_desc_bf16(128 * CG, kTileN, A_MN, B_MN);
+            constexpr uint32_t a_step = A_MN ? 16 * 128 : 32, b_step = B_MN ? 16 * 128 : 32;      // bytes from one K of 16 to the next
+            int s = 0, acc = 0; uint32_t ph = 0, aph = 0; bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+                const int steps = (q.k1 - q.k0) * a.pairs;
+                for (int i0 = 0; i0 < steps && ok; i0 += kSegment) {
+                    const int i1 = min(steps, i0 + kSegment);
+                    if (!mbar_wait(tempty(acc), aph ^ 1u, gave_up)) { ok = false; break; }
+                    fence_after_sync();
+                    const uint32_t d = tmem + acc * kTileN;
+                    for (int i = i0; i < i1; ++i) {
+                        if (!mbar_wait(full(s), ph, gave_up)) { ok = false; break; }
+                        fence_after_sync();
+                        const uint32_t sa = base + s * SB;
+                        const uint64_t da = smem_desc(sa, A_MN ? 8192 : 16, 1024), db = smem_desc(sa + 16384, B_MN ? 8192 : 16, 1024);
+#pragma unroll
+                        for (int j = 0; j < kTileK / 16; ++j)
+                            mma_bf16<CG>(d, da + j * (a_step >> 4), db + j * (b_step >> 4), idesc, i != i0 || j != 0);
+                        mma_commit<CG>(empty(s));
+                        if (++s == NS) { s = 0; ph ^= 1u; }
+                    }
+                    if (!ok) break;
+                    mma_commit<CG>(tfull(acc));
+                    if (++acc == 2) { acc = 0; aph ^= 1u; }
+                }
+            }
+            mma_commit<CG>(drain);                       // nothing may be in flight when tensor memory is given back
+            int quiet = 0;
+            mbar_wait(drain, 0, &quiet);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");   // 128 x 40 + 256 x 232 = 384 x 168, what the block was launched with
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        float* const stage = staging + (warp - 4) * kPiece * 32 + lane;       // [column][lane]
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const float alpha = (KIND == kGradW && a.scale != 0.0f) ? a.scale / (float)max(count, 1) : 1.0f;
+        int acc = 0; uint32_t aph = 0; bool ok = true;
+        for (int t = first; t < tiles && ok; t += step) {
+            const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+            const int r = q.m * 128 * CG + (int)rank * 128 + quarter * 32 + lane;     // the thread's row of the tile's M axis
+            const int col = q.n * kTileN + half * kHalf;                              // its first column
+            const int have = a.cols - col;                                            // columns that exist
+            // targets of the row: the first one not before the half tile
+            int64_t e0 = 0; int pos = 0, next = INT32_MAX; const int ke = a.k > 0 ? a.k : 1, v_at = a.v0 + col;
+            float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if ((KIND == kLse || KIND == kProb) && r < count) {
+                e0 = (int64_t)w.map[r] * ke;
+                int lo = 0, hi = ke;
+                while (lo < hi) { const int mid = (lo + hi) >> 1; if (a.eidx[e0 + mid] < v_at) lo = mid + 1; else hi = mid; }
+                pos = lo;
+                if (pos < ke) next = a.eidx[e0 + pos];
+                if (KIND == kProb) rc = w.rowc[r];
+            }
+            float f[kHalf];
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) f[j] = 0.0f;
+            const int steps = (q.k1 - q.k0) * a.pairs;
+            for (int i0 = 0; i0 < steps; i0 += kSegment) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(tfull(acc), aph, gave_up))) { ok = false; break; }    // the warp leaves as one
+                fence_after_sync();
+                const uint32_t d = tmem + lanes + acc * kTileN + half * kHalf;
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(d + c, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[c + j] += __uint_as_float(v[j]);
+                }
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty(acc), 0));
+                if (++acc == 2) { acc = 0; aph ^= 1u; }
+            }
+            if (!ok) break;
+
+            if (KIND == kLse) {
+#pragma unroll
+                for (int c = 0; c < kHalf; c += kPiece) {
+                    if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
+#pragma unroll
+                        for (int j = 0; j < kPiece; ++j) stage[j * 32] = f[c + j];
+                        while (next < v_at + c + kPiece) {
+                            w.zt[e0 + pos] = stage[(next - v_at - c) * 32];
+                            next = ++pos < ke ? a.eidx[e0 + pos] : INT32_MAX;
+                        }
+                    }
+                }
+                if (have < kHalf) {
+#pragma unroll
+                    for (int j = 0; j < kHalf; ++j) if (j >= have) f[j] = -INFINITY;
+                }
+                float m0 = f[0], m1 = f[1], m2 = f[2], m3 = f[3];
+#pragma unroll
+                for (int j = 4; j < kHalf; j += 4) { m0 = fmaxf(m0, f[j]); m1 = fmaxf(m1, f[j + 1]); m2 = fmaxf(m2, f[j + 2]); m3 = fmaxf(m3, f[j + 3]); }
+                const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * a.c2, off = m == -INFINITY ? 0.0f : m;
+                float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kHalf; j += 4) {
+                    s0 += ex2(__fmaf_rn(f[j], a.c2, -off)); s1 += ex2(__fmaf_rn(f[j + 1], a.c2, -off));
+                    s2 += ex2(__fmaf_rn(f[j + 2], a.c2, -off)); s3 += ex2(__fmaf_rn(f[j + 3], a.c2, -off));
+                }
+                if (r < count) w.part[(int64_t)r * w.parts + 2 * q.n + half] = make_float2(m, (s0 + s1) + (s2 + s3));
+            } else if (KIND == kProb) {
+                __nv_bfloat16* o = w.g + (int64_t)r * w.vc + col;
+#pragma unroll
+                for (int c = 0; c < kHalf; c += kPiece) {
+#pragma unroll
+                    for (int j = c; j < c + kPiece; ++j)
+                        f[j] = (r < count && j < have) ? rc.y * ex2(__fmaf_rn(f[j], a.c2, -rc.x)) : 0.0f;
+                    if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
+#pragma unroll
+                        for (int j = 0; j < kPiece; ++j) stage[j * 32] = f[c + j];
+                        while (next < v_at + c + kPiece) {
+                            stage[(next - v_at - c) * 32] -= (a.k > 0 ? w.eq[e0 + pos] : 1.0f) * rc.z;
+                            next = ++pos < ke ? a.eidx[e0 + pos] : INT32_MAX;
+                        }
+#pragma unroll
+                        for (int j = 0; j < kPiece; ++j) f[c + j] = stage[j * 32];
+                    }
+                    store_terms<F32 ? 3 : 1>(o + c, w.n_pad * w.vc, f + c, true);
+                }
+            } else if (KIND == kGradH) {
+                if (r < count) {
+                    float* o = w.dh + ((int64_t)q.split * w.n_pad + r) * w.dq + col;
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += 8) {
+                        if (col + c < w.dq) {
+                            float x[8], y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = f[c + j];
+                            if (!a.first) {
+                                load8_rw(o + c, y);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) x[j] += y[j];
+                            }
+                            store8(o + c, x);
+                        }
+                    }
+                }
+            } else if (r < mdim) {
+                const int64_t at = (int64_t)(a.v0 + r) * a.ld + col;
+                if (KIND == kGradW && alpha != 1.0f) {
+#pragma unroll
+                    for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
+                }
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 16) {
+                    if (a.align && c + 16 <= have) {
+                        if (F32) {
+                            uint32_t x[8], y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) { x[j] = __float_as_uint(f[c + j]); y[j] = __float_as_uint(f[c + 8 + j]); }
+                            store32(static_cast<float*>(a.out) + at + c, x, a.align == 2);
+                            store32(static_cast<float*>(a.out) + at + c + 8, y, a.align == 2);
+                        } else {
+                            store_terms<1>(static_cast<__nv_bfloat16*>(a.out) + at + c, 0, f + c, a.align == 2);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = c; j < c + 16; ++j) {
+                            if (j < have) {
+                                if (F32) static_cast<float*>(a.out)[at + j] = f[j];
+                                else static_cast<__nv_bfloat16*>(a.out)[at + j] = __float2bfloat16_rn(f[j]);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && *gave_up) set_status(&w.ctrl->status, DQ_ERR_TIMEOUT);
+    fence_before_sync();
+    if (CG == 2) cluster_sync();
+    fence_after_sync();
+    if (warp == 2) tmem_free<CG>(tmem, 512);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static EncodeTiled fn = [] {
+        void* p = nullptr; cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) { cudaGetLastError(); p = nullptr; }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Tensor map of `planes` matrices of bf16 rows; boxes of 64 values by `box` rows.  Values outside read as zero.
+bool make_map(CUtensorMap* map, const void* p, int64_t inner, int64_t rows, int64_t pitch, int planes, int64_t plane, int box)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)plane * 2};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+    EncodeTiled f = encode_tiled();
+    return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Device { int id = -1, sms = 0; };
+bool device(Device* d)
+{
+    static thread_local Device last;
+    int id = 0;
+    if (cudaGetDevice(&id) != cudaSuccess) return false;
+    if (id != last.id) {
+        int sms = 0;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, id) != cudaSuccess) return false;
+        last.id = id; last.sms = sms;
+    }
+    *d = last;
+    return true;
+}
+
+template <int CG, int KIND, bool F32>
+bool launch_mma_cg(const CUtensorMap& ma, const CUtensorMap& mb, const MmaArgs& a, const Work& w, int64_t tiles, int sms, cudaStream_t st)
+{
+    auto kernel = vocab_mma_kernel<CG, KIND, F32>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<CG>()) != cudaSuccess) return false;
+    const int64_t units = sms / CG;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(CG * (tiles < units ? tiles : units))); cfg.blockDim = dim3(384);
+    cfg.dynamicSmemBytes = smem_bytes<CG>(); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, a, w) == cudaSuccess;
+}
+
+// m: extent of the tile's M axis, nt: tiles along N (times splits).  The columns' operand comes in boxes of 256 / CG rows where it is
+// K-major: `mb` for one CTA, `mb2` for a pair.
+template <int KIND, bool F32>
+bool launch_mma(int64_t m, int64_t nt, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mb2, const MmaArgs& a, const Work& w, int sms,
+                cudaStream_t st)
+{
+    if (row_pairs(m) == 2) return launch_mma_cg<2, KIND, F32>(ma, mb2, a, w, (m + 255) / 256 * nt, sms, st);
+    return launch_mma_cg<1, KIND, F32>(ma, mb, a, w, nt, sms, st);
+}
+
+struct Targets { const int32_t* labels; const int32_t* top_idx; const float* top_logits; const float* teacher_lse; float temp; };
+struct Grads { const float* weight; void* gh; int64_t ld_h; void* gw; int64_t ld_w; };
+
+template <bool F32>
+int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
+{
+    const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2;
+    const int64_t n = v->n, V = v->V;
+    const int blocks = dev.sms * 8;
+    auto grid8 = [&](int64_t rows) { return dim3((unsigned)min((int64_t)blocks, (rows + 7) / 8)); };
+    bool ok = true;
+    if (k > 0)
+        ok = ok && launch_k(vocab_targets_kernel, dim3((unsigned)min((int64_t)blocks, (n + 3) / 4)), dim3(128), 0, st, t.top_idx, t.top_logits, t.teacher_lse,
+                            1.0f / t.temp, n, k, V, w) == cudaSuccess;
+    const int64_t gblocks = min((int64_t)dev.sms * 2, (n + 7) / 8), per = (n + gblocks - 1) / gblocks;
+    ok = ok && launch_k(vocab_gather_kernel<F32>, dim3((unsigned)((n + per - 1) / per)), dim3(256), 0, st, v->h, v->ld_h, d, k > 0 ? w.tgt : t.labels,
+                        V, n, per, ptr_aligned(v->h, 16) && v->ld_h * elem % 16 == 0, loss, lse, w) == cudaSuccess;
+    if (!w.direct_w)
+        ok = ok && launch_k(vocab_weights_kernel<F32>, grid8(V), dim3(256), 0, st, v->w, v->ld_w, d, V, ptr_aligned(v->w, 16) && v->ld_w * elem % 16 == 0, w) == cudaSuccess;
+    const __nv_bfloat16* wsrc = w.direct_w ? static_cast<const __nv_bfloat16*>(v->w) : w.wp;
+    const int64_t wpitch = w.direct_w ? v->ld_w : w.dp;
+
+    MmaArgs a = {};
+    a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
+    a.splits = 1; a.kps = 0; a.scale = g && !g->weight ? t.temp : 0.0f;
+    CUtensorMap mh, mw, mw2;
+    ok = ok && make_map(&mh, w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128);
+    ok = ok && make_map(&mw, wsrc, d, V, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wsrc, d, V, wpitch, T, V * wpitch, kTileN / 2);
+    if (!ok) return DQ_ERR_CUDA;
+    a.cols = (int)V; a.kdim = d;
+    ok = launch_mma<kLse, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
+    ok = ok && launch_k(vocab_join_kernel, grid8(n), dim3(256), 0, st, w, k, t.labels, g ? g->weight : (const float*)nullptr, t.temp, a.c2, loss, lse) == cudaSuccess;
+    if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
+
+    CUtensorMap mg_k, mg_mn, mw_mn, mh_mn;
+    const int ntd = (d + kTileN - 1) / kTileN;
+    ok = ok && make_map(&mg_k, w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128);
+    ok = ok && make_map(&mg_mn, w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK);
+    ok = ok && make_map(&mh_mn, w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
+    for (int64_t v0 = 0; v0 < V && ok; v0 += w.vc) {
+        const int vn = (int)min(w.vc, V - v0);
+        const __nv_bfloat16* wv = wsrc + v0 * wpitch;
+        ok = make_map(&mw, wv, d, vn, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wv, d, vn, wpitch, T, V * wpitch, kTileN / 2) &&
+             make_map(&mw_mn, wv, d, vn, wpitch, T, V * wpitch, kTileK);
+        a.v0 = (int)v0; a.cols = vn; a.kdim = d; a.splits = 1;
+        ok = ok && launch_mma<kProb, F32>(n, (vn + kTileN - 1) / kTileN, mh, mw, mw2, a, w, dev.sms, st);
+        a.cols = d; a.mdim = vn; a.out = g->gw; a.ld = g->ld_w; a.align = !ptr_aligned(g->gw, 16) || g->ld_w * elem % 16 ? 0 : !ptr_aligned(g->gw, 32) || g->ld_w * elem % 32 ? 1 : 2;
+        ok = ok && launch_mma<kGradW, F32>(vn, ntd, mg_mn, mh_mn, mh_mn, a, w, dev.sms, st);
+        a.kdim = vn; a.kps = w.kps; a.first = v0 == 0;
+        a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
+        ok = ok && launch_mma<kGradH, F32>(n, (int64_t)ntd * a.splits, mg_k, mw_mn, mw_mn, a, w, dev.sms, st);
+    }
+    ok = ok && launch_k(vocab_grad_h_kernel<F32>, grid8(n), dim3(256), 0, st, w, n, d, a.scale, g->gh, g->ld_h) == cudaSuccess;
+    return ok ? DQ_OK : DQ_ERR_CUDA;
+}
+
+int check_vocab(const dq_vocab* v)
+{
+    if (!v) return DQ_ERR_ARG;
+    if (v->format != DQ_DENSE_F32 && v->format != DQ_DENSE_BF16) return DQ_ERR_ARG;
+    if (v->n < 0 || v->n > (1 << 24) || v->d < 1 || v->d > (1 << 16) || v->V < 1 || v->V > (1 << 28) || v->k < 0 || v->k > kMaxTop) return DQ_ERR_ARG;
+    if (v->ld_h < v->d || v->ld_w < v->d || v->ld_h > ((int64_t)1 << 32) || v->ld_w > ((int64_t)1 << 32)) return DQ_ERR_ARG;
+    return DQ_OK;
+}
+
+int run(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, void* stream)
+{
+    int rc = check_vocab(v);
+    if (rc != DQ_OK) return rc;
+    const int elem = v->format == DQ_DENSE_F32 ? 4 : 2;
+    if (!v->w || !v->workspace || !ptr_aligned(v->w, elem) || !ptr_aligned(v->workspace, 256)) return DQ_ERR_ARG;
+    if (v->n > 0 && (!v->h || !loss || !ptr_aligned(v->h, elem) || !ptr_aligned(loss, 4) || !ptr_aligned(lse, 4))) return DQ_ERR_ARG;
+    if (g) {
+        if (!g->gw || (v->n > 0 && !g->gh) || !ptr_aligned(g->gw, elem) || !ptr_aligned(g->gh, elem) || !ptr_aligned(g->weight, 4)) return DQ_ERR_ARG;
+        if (g->ld_h < v->d || g->ld_w < v->d) return DQ_ERR_ARG;
+    }
+    if (!(t.temp > 0.0f) || !isfinite(t.temp)) return DQ_ERR_ARG;
+    Device dev;
+    if (!device(&dev)) { cudaGetLastError(); return DQ_ERR_CUDA; }
+    const Work w = carve(v, g != nullptr, dev.sms);
+    if (v->workspace_bytes < w.bytes) return DQ_ERR_SHAPE;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (v->n == 0) {                                     // no rows: no losses, a zero gradient of the weights
+        if (cudaMemsetAsync(w.ctrl, 0, sizeof(Ctrl), st) != cudaSuccess) return DQ_ERR_CUDA;
+        if (g && cudaMemset2DAsync(g->gw, (size_t)g->ld_w * elem, 0, (size_t)v->d * elem, (size_t)v->V, st) != cudaSuccess) return DQ_ERR_CUDA;
+        return DQ_OK;
+    }
+    rc = v->format == DQ_DENSE_F32 ? run_loss<true>(v, t, loss, lse, g, w, dev, st) : run_loss<false>(v, t, loss, lse, g, w, dev, st);
+    if (rc != DQ_OK) cudaGetLastError();
+    return rc;
+}
+
+}  // namespace
+}  // namespace dq
+
+using namespace dq;
+
+extern "C" {
+
+int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
+{
+    Device dev;
+    if (check_vocab(v) != DQ_OK) return -1;
+    if (!device(&dev)) { cudaGetLastError(); return -1; }
+    return carve(v, grad != 0, dev.sms).bytes;
+}
+
+int dq_xent_loss(const dq_vocab* v, const int32_t* labels, float* loss, float* lse, void* stream)
+{
+    if (!v || v->k != 0 || (v->n > 0 && !labels) || !ptr_aligned(labels, 4)) return DQ_ERR_ARG;
+    return run(v, Targets{labels, nullptr, nullptr, nullptr, 1.0f}, loss, lse, nullptr, stream);
+}
+
+int dq_xent_grad(const dq_vocab* v, const int32_t* labels, const float* weight, float* loss, float* lse, void* grad_h, int64_t ld_gh,
+                 void* grad_w, int64_t ld_gw, void* stream)
+{
+    if (!v || v->k != 0 || (v->n > 0 && !labels) || !ptr_aligned(labels, 4)) return DQ_ERR_ARG;
+    const Grads g = {weight, grad_h, ld_gh, grad_w, ld_gw};
+    return run(v, Targets{labels, nullptr, nullptr, nullptr, 1.0f}, loss, lse, &g, stream);
+}
+
+int dq_distill_loss(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,
+                    float* loss, float* lse, void* stream)
+{
+    if (!v || v->k < 1 || (v->n > 0 && (!top_idx || !top_logits))) return DQ_ERR_ARG;
+    if (!ptr_aligned(top_idx, 4) || !ptr_aligned(top_logits, 4) || !ptr_aligned(teacher_lse, 4)) return DQ_ERR_ARG;
+    return run(v, Targets{nullptr, top_idx, top_logits, teacher_lse, temperature}, loss, lse, nullptr, stream);
+}
+
+int dq_distill_grad(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,
+                    const float* weight, float* loss, float* lse, void* grad_h, int64_t ld_gh, void* grad_w, int64_t ld_gw, void* stream)
+{
+    if (!v || v->k < 1 || (v->n > 0 && (!top_idx || !top_logits))) return DQ_ERR_ARG;
+    if (!ptr_aligned(top_idx, 4) || !ptr_aligned(top_logits, 4) || !ptr_aligned(teacher_lse, 4)) return DQ_ERR_ARG;
+    const Grads g = {weight, grad_h, ld_gh, grad_w, ld_gw};
+    return run(v, Targets{nullptr, top_idx, top_logits, teacher_lse, temperature}, loss, lse, &g, stream);
+}
+
+int dq_vocab_status(const dq_vocab* v, int* status, void* stream)
+{
+    if (!v || !v->workspace || !status) return DQ_ERR_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (cudaMemcpyAsync(status, &static_cast<const Ctrl*>(v->workspace)->status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) { cudaGetLastError(); return DQ_ERR_CUDA; }
+    return DQ_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,476 @@
+"""The vocabulary losses on the GPU against their definitions in 64 bits.
+
+Tolerances, elementwise, from the arithmetic (u = 2^-24, the rounding of fp32):
+  logits    products of bf16 values (or of fp32 values as three bf16 terms) are exact; a sum runs over segments of 512 in the
+            tensor cores, which cut off toward zero at each of 32 steps (and align the 16 products of a step): at most
+            2 * 32 * 2u of A = sum |h_i w_i|, six times as many steps for the fp32 terms, plus one rounding per segment.
+  lse       moves by no more than the largest logit error; exp2 is good to 4u, the sum of up to V terms of one sign adds
+            no more than 8u in total along any tree used here (128 terms as four chains of 32, then pairs), log and the
+            final rounding 2u |lse|.
+  gradient  g = weight T (S p - q) has the relative error of p: the logit error of the label's row / T twice (z and lse),
+            plus 2^-8 relative where it is rounded to bf16 (3 terms for fp32: 2^-24).  A product adds the segment error
+            above, relative to |g| |w|, and the output's rounding: half a step of its type.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def dq():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    import paper_1805_10111_b200 as m
+    m.lib()
+    return m
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _sum_err(K, f32):
+    """Relative to the sum of magnitudes: tensor-core segments, then one rounding per segment."""
+    pairs = 6 if f32 else 1
+    steps = -(-K // 64) * 4 * pairs
+    return 2 * 2 * U * min(32, steps) + U * -(-steps // 32) + (4 * U if f32 else 0)
+
+
+class Ref:
+    """Losses and gradients in 64 bits, with the bounds of the module's docstring.  entries: (idx, q, logq, there), each [n, k]."""
+
+    def __init__(self, h, w, idx, q, logq, there, T=1.0, weight=None, f32=False):
+        torch = _torch()
+        n, d = h.shape
+        self.has = there.any(1)
+        H, W = torch.where(self.has[:, None], h.double(), 0.0), w.double()
+        z = H @ W.t() / T
+        zerr = (H.abs() @ W.abs().t() / T).max(1).values * _sum_err(d, f32) + z.abs().max(1).values * 2 * U      # c = 1/T is rounded too
+        self.lse = torch.logsumexp(z, 1)
+        at = torch.where(there, idx, 0).long()
+        zt = z.gather(1, at)
+        self.loss = T * T * torch.where(there & (q > 0), q * (logq - (zt - self.lse[:, None])), 0.0).sum(1)
+        lse_err = zerr + 12 * U + 2 * U * self.lse.abs()
+        mass = q.sum(1)
+        self.loss_err = T * T * (mass * (zerr + lse_err) + 8 * U * (q * (logq.abs() + zt.abs() + self.lse.abs()[:, None])).sum(1)) + 2 * U * self.loss.abs()
+        self.lse_err = lse_err
+        for name in ("lse", "loss", "lse_err", "loss_err"):
+            setattr(self, name, torch.where(self.has, getattr(self, name), 0.0))
+        wt = weight.double() if weight is not None else torch.full((n,), 1.0 / max(1, int(self.has.sum())), dtype=torch.float64, device=h.device)
+        self.wt = torch.where(self.has, wt, 0.0) * T
+        p = torch.exp(z - self.lse[:, None])
+        g = (mass[:, None] * p).scatter_add_(1, at, -q) * self.wt[:, None]
+        # |g| error: of p and q each by relative error, and the rounding
+        pe = (mass[:, None] * p) * (2 * zerr + 24 * U + 4 * U * self.lse.abs())[:, None] + 2.0 ** -125        # exp2 flushes below 2^-126
+        qe = torch.zeros_like(p).scatter_add_(1, at, q * (8 * U * (1 + logq.abs())))
+        ge = (pe + qe) * self.wt.abs()[:, None] + g.abs() * (2 * U if f32 else 2.0 ** -8 * 1.01)
+        gm = (mass[:, None] * p + torch.zeros_like(p).scatter_add_(1, at, q)) * self.wt.abs()[:, None]      # terms before they cancel
+        half = U if f32 else 2.0 ** -8
+        self.gh, self.gw = g @ W, g.t() @ H
+        tiny = 2.0 ** -133 if not f32 else 2.0 ** -149                    # half a step of the smallest values
+        self.gh_err = 1.01 * (ge @ W.abs() + (g.abs() @ W.abs()) * (_sum_err(w.shape[0], f32) + 8 * U) + gm @ W.abs() * 2 * U) + self.gh.abs() * half * 1.01 + tiny
+        self.gw_err = 1.01 * (ge.t() @ H.abs() + (g.abs().t() @ H.abs()) * (_sum_err(n, f32) + 8 * U) + gm.t() @ H.abs() * 2 * U) + self.gw.abs() * half * 1.01 + tiny
+
+    def check(self, loss=None, lse=None, gh=None, gw=None, where=""):
+        torch = _torch()
+        for name, got, want, err in (("loss", loss, self.loss, self.loss_err), ("lse", lse, self.lse, self.lse_err),
+                                     ("grad_h", gh, getattr(self, "gh", None), getattr(self, "gh_err", None)),
+                                     ("grad_w", gw, getattr(self, "gw", None), getattr(self, "gw_err", None))):
+            if got is None:
+                continue
+            off = (got.double() - want).abs()
+            assert torch.isfinite(off).all(), (where, name, "not finite")
+            worst = (off / err.clamp(min=1e-300)).max().item() if off.numel() and off.max() > 0 else 0.0
+            assert worst <= 1.0, (where, name, "error over its bound by", worst)
+
+
+def xent_ref(h, w, labels, weight=None):
+    torch = _torch()
+    there = ((labels >= 0) & (labels < w.shape[0]))[:, None]
+    one = there.double()
+    return Ref(h, w, labels[:, None], one, torch.zeros_like(one), there, 1.0, weight, h.dtype == torch.float32)
+
+
+def distill_ref(h, w, idx, t, teacher_lse=None, T=1.0, weight=None):
+    torch = _torch()
+    there = (idx >= 0) & (idx < w.shape[0]) & (t != -math.inf)
+    t = torch.where(there, t.double() / T, -math.inf)
+    tl = teacher_lse.double() if teacher_lse is not None else torch.logsumexp(torch.where(there.any(1)[:, None], t, 0.0), 1)
+    logq = torch.where(there, t - tl[:, None], 0.0)
+    q = torch.where(there, logq.exp(), 0.0)
+    return Ref(h, w, idx, q, logq, there, T, weight, h.dtype == torch.float32)
+
+
+def _inputs(n, d, V, dt, seed, scale=2.0):
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    w = (torch.randn(V, d, generator=g, device="cuda") * (scale / math.sqrt(d))).to(dt)
+    labels = torch.randint(0, V, (n,), generator=g, device="cuda")
+    h = (torch.randn(n, d, generator=g, device="cuda") + w[labels].float()).to(dt)
+    return g, h, w, labels.int()
+
+
+def _entries(g, n, V, k, labels):
+    torch = _torch()
+    idx = torch.randint(0, V, (n, k), generator=g, device="cuda").int()             # classes may repeat
+    idx[:, k // 2] = labels
+    t = torch.randn(n, k, generator=g, device="cuda") * 2
+    return idx, t
+
+
+def _outputs(h, w, fill=float("nan")):
+    torch = _torch()
+    n = h.shape[0]
+    return [torch.full((n,), fill, device="cuda"), torch.full((n,), fill, device="cuda"), torch.full(h.shape, fill, dtype=h.dtype, device="cuda"),
+            torch.full(w.shape, fill, dtype=w.dtype, device="cuda")]
+
+
+def _layer(dq, h, w, k=0, grad=True):
+    """A holder whose workspace starts as NaN patterns: nothing may be read that the call did not write."""
+    layer = dq.Vocab(h, w, k=k, grad=grad)
+    layer.workspace.fill_(255)
+    return layer
+
+
+def xent(dq, h, w, labels, weight=None):
+    layer = _layer(dq, h, w)
+    loss, lse, gh, gw = _outputs(h, w)
+    assert dq.dq_xent_grad(layer, labels, weight, loss, lse, gh, gw) == 0
+    assert dq.dq_vocab_status(layer) == (0, 0)
+    return loss, lse, gh, gw
+
+
+def distill(dq, h, w, idx, t, tl=None, T=1.0, weight=None):
+    layer = _layer(dq, h, w, k=idx.shape[1])
+    loss, lse, gh, gw = _outputs(h, w)
+    assert dq.dq_distill_grad(layer, idx, t, tl, T, weight, loss, lse, gh, gw) == 0
+    assert dq.dq_vocab_status(layer) == (0, 0)
+    return loss, lse, gh, gw
+
+
+SHAPES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (20, 100, 10), (64, 64, 129), (127, 64, 255), (128, 72, 256), (129, 65, 257), (200, 513, 1000),
+          (256, 1032, 300), (257, 40, 5000), (1, 2048, 3001), (700, 1100, 515)]
+TYPES = ["bfloat16", "float32"]
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("n,d,V", SHAPES)
+def test_cross_entropy(dq, n, d, V, dt):
+    torch = _torch()
+    g, h, w, labels = _inputs(n, d, V, getattr(torch, dt), n + d)
+    weight = torch.rand(n, generator=g, device="cuda") - 0.25 if n % 2 else None
+    if n > 4:
+        labels[torch.randperm(n, generator=g, device="cuda")[:n // 4]] = -100
+    ref = xent_ref(h, w, labels, weight)
+    ref.check(*xent(dq, h, w, labels, weight))
+    layer = _layer(dq, h, w, grad=False)
+    loss, lse = _outputs(h, w)[:2]
+    assert dq.dq_xent_loss(layer, labels, loss, lse) == 0
+    ref.check(loss, lse)
+    loss.fill_(float("nan"))
+    assert dq.dq_xent_loss(layer, labels, loss) == 0                       # lse is optional
+    ref.check(loss)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("n,d,V", SHAPES)
+@pytest.mark.parametrize("k,T,tail", [(1, 1.0, False), (9, 2.0, True), (64, 1.5, False)])
+def test_distillation(dq, n, d, V, dt, k, T, tail):
+    torch = _torch()
+    g, h, w, labels = _inputs(n, d, V, getattr(torch, dt), n + d + k)
+    idx, t = _entries(g, n, V, k, labels)
+    if n > 4:
+        gone = torch.randperm(n, generator=g, device="cuda")
+        idx[gone[:n // 5]] = -1
+        idx[gone[n // 5:n // 2], k // 2 + 1:] = V                            # lists of another length
+        t[gone[n // 2:n // 2 + 2], 0] = -math.inf
+    tl = torch.logsumexp(t / T, 1) + torch.rand(n, generator=g, device="cuda") if tail else None
+    weight = torch.rand(n, generator=g, device="cuda") if n % 2 else None
+    ref = distill_ref(h, w, idx, t, tl, T, weight)
+    ref.check(*distill(dq, h, w, idx, t, tl, T, weight))
+    layer = _layer(dq, h, w, k=k, grad=False)
+    loss, lse = _outputs(h, w)[:2]
+    assert dq.dq_distill_loss(layer, idx, t, tl, T, loss, lse) == 0
+    ref.check(loss, lse)
+
+
+def test_longest_list_and_one_class_many_times(dq):
+    torch = _torch()
+    g, h, w, labels = _inputs(40, 48, 300, torch.float32, 3)
+    idx, t = _entries(g, 40, 300, 256, labels)
+    idx[3] = 17                                                              # 256 entries of one class
+    idx[4] = torch.randperm(300, device="cuda")[:256].int()
+    distill_ref(h, w, idx, t, None, 2.0).check(*distill(dq, h, w, idx, t, None, 2.0))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_rows_without_a_target_may_hold_anything(dq, dt):
+    torch = _torch()
+    g, h, w, labels = _inputs(300, 72, 500, getattr(torch, dt), 5)
+    for i, bad in enumerate((-1, 500, 2 ** 31 - 1, -2 ** 31)):
+        labels[i::11] = bad
+    empty = (labels < 0) | (labels >= 500)
+    h[empty] = torch.tensor([float("nan"), float("inf")] * 36, device="cuda").to(h.dtype)
+    ref = xent_ref(h, w, labels)
+    out = xent(dq, h, w, labels)
+    ref.check(*out)
+    assert not out[0][empty].any() and not out[1][empty].any() and not out[2][empty].any()
+    idx, t = _entries(g, 300, 500, 6, labels)
+    idx[empty] = -1
+    idx[7], t[7] = 3, -math.inf                                             # present classes, no logit left
+    out = distill(dq, h, w, idx, t)
+    distill_ref(h, w, idx, t).check(*out)
+    assert out[0][7] == 0 and not out[2][7].any()
+
+
+@pytest.mark.parametrize("n", [0, 1, 200])
+@pytest.mark.parametrize("dt", TYPES)
+def test_no_row_with_a_target(dq, n, dt):
+    torch = _torch()
+    h = torch.full((n, 40), float("nan"), device="cuda").to(getattr(torch, dt))
+    w = torch.randn(300, 40, device="cuda").to(h.dtype)
+    loss, lse, gh, gw = xent(dq, h, w, torch.full((n,), -1, dtype=torch.int32, device="cuda"))
+    assert not loss.any() and not lse.any() and not gh.any() and not gw.any()
+    loss, lse, gh, gw = distill(dq, h, w, torch.full((n, 3), -1, dtype=torch.int32, device="cuda"), torch.zeros(n, 3, device="cuda"))
+    assert not loss.any() and not lse.any() and not gh.any() and not gw.any()
+
+
+def test_non_finite_values_spread_as_the_formulas_say(dq):
+    torch = _torch()
+    _, h, w, labels = _inputs(150, 64, 300, torch.bfloat16, 6)
+    h[10, 3] = float("nan")
+    loss, lse, gh, gw = xent(dq, h, w, labels)
+    bad = torch.zeros(150, dtype=torch.bool, device="cuda"); bad[10] = True
+    assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(lse), bad) and torch.equal(torch.isnan(gh).any(1), bad)
+    assert torch.isnan(gw).all()
+    _, h, w, labels = _inputs(150, 64, 300, torch.bfloat16, 6)
+    idx, t = labels[:, None].repeat(1, 2).contiguous(), torch.zeros(150, 2, device="cuda")
+    t[5, 1] = float("nan")
+    loss, lse, gh, gw = distill(dq, h, w, idx, t)
+    assert torch.isnan(loss[5]) and torch.isfinite(lse).all() and torch.isnan(loss).sum() == 1 and torch.isnan(gh[5]).all()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_large_logits(dq, dt):
+    """Logits of several hundred: exp overflows without the running maximum; most probabilities underflow to zero."""
+    torch = _torch()
+    _, h, w, labels = _inputs(140, 64, 700, getattr(torch, dt), 8, scale=2.0)
+    h = (h.float() * 100).to(h.dtype)
+    xent_ref(h, w, labels).check(*xent(dq, h, w, labels))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("off,pad", [(0, 8), (1, 7), (8, 16), (3, 0)])
+def test_strides_and_alignment(dq, dt, off, pad):
+    """Rows that start anywhere: inputs and gradients are windows of wider arrays, whose other values stay as they were."""
+    torch = _torch()
+    g, h0, w0, labels = _inputs(150, 72, 260, getattr(torch, dt), 9)
+    wide = 72 + off + pad
+
+    def window(x):
+        big = torch.full((x.shape[0] + 2, wide), 7.0, dtype=x.dtype, device="cuda")
+        big[1:-1, off:off + 72] = x
+        return big, big[1:-1, off:off + 72]
+
+    (bh, h), (bw, w) = window(h0), window(w0)
+    (bgh, gh), (bgw, gw) = window(torch.zeros_like(h0)), window(torch.zeros_like(w0))
+    layer = _layer(dq, h, w)
+    loss, lse = _outputs(h, w)[:2]
+    assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh, gw) == 0
+    xent_ref(h0, w0, labels).check(loss, lse, gh, gw)
+    for big, x in ((bgh, gh), (bgw, gw), (bh, h), (bw, w)):
+        x.zero_()
+        big[1:-1, off:off + 72] = 7.0
+        assert (big == 7.0).all()
+
+
+def test_pieces_of_the_vocabulary(dq):
+    """Enough rows and classes that the gradient of the logits is formed in several pieces, the last one ragged."""
+    torch = _torch()
+    for dt, n, V in ((torch.bfloat16, 2047, 140001), (torch.float32, 1030, 40003)):
+        _, h, w, labels = _inputs(n, 24, V, dt, 10)
+        labels[:2] = torch.tensor([V - 1, 0])
+        xent_ref(h, w, labels).check(*xent(dq, h, w, labels))
+
+
+def test_offsets_past_32_bits(dq):
+    """Weights and their gradient of more than 2^31 values: the last classes are the last rows of memory."""
+    torch = _torch()
+    n, d, V = 3, 4096, 600_000
+    w = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, V, 50_000):
+        w[i:i + 50_000] = torch.randn(50_000, d, device="cuda") * (1.0 / 64)
+    h = torch.randn(n, d, device="cuda").bfloat16()
+    labels = torch.tensor([V - 1, 550_000, 0], dtype=torch.int32, device="cuda")
+    layer = dq.Vocab(h, w)
+    loss, lse = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    gh, gw = torch.empty_like(h), torch.empty_like(w)
+    assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh, gw) == 0
+    H = h.double()
+    z = torch.cat([H @ w[i:i + 50_000].double().t() for i in range(0, V, 50_000)], 1)
+    want = torch.logsumexp(z, 1)
+    A = max((H.abs() @ w[i:i + 50_000].double().abs().t()).max().item() for i in range(0, V, 50_000))
+    tol = A * _sum_err(d, False) + (24 + 4 * want.abs().max().item()) * U
+    assert (lse.double() - want).abs().max() <= tol
+    assert (loss.double() - (want - z.gather(1, labels.long()[:, None])[:, 0])).abs().max() <= 2 * tol
+    p = torch.exp(z - want[:, None])
+    p[torch.arange(n), labels.long()] -= 1
+    p /= n
+    for i in (0, 250_000, V - 1000):
+        at = slice(i, i + 1000)
+        ref, mag = p[:, at].t() @ H, p[:, at].abs().t() @ H.abs()
+        assert ((gw[at].double() - ref).abs() <= mag * (2.0 ** -8 * 1.02 + 4 * tol) + ref.abs() * 2.0 ** -8 * 1.01 + 2.0 ** -133).all(), i
+
+
+def test_equal_inputs_give_equal_bytes(dq):
+    torch = _torch()
+    g, h, w, labels = _inputs(900, 200, 3000, torch.bfloat16, 12)
+    idx, t = _entries(g, 900, 3000, 20, labels)
+    a, b = xent(dq, h, w, labels), xent(dq, h, w, labels)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    a, b = distill(dq, h, w, idx, t, None, 2.0), distill(dq, h, w, idx, t, None, 2.0)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_graph_replay_streams_and_reused_workspace(dq):
+    """One holder called for smaller and larger work in turn, captured into a graph and replayed on new inputs while another
+    holder's calls run on a second stream."""
+    torch = _torch()
+    _, h, w, labels = _inputs(400, 128, 2000, torch.bfloat16, 13)
+    layer = dq.Vocab(h, w)
+    out = _outputs(h, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        assert dq.dq_xent_grad(layer, labels, None, *out) == 0
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            assert dq.dq_xent_grad(layer, labels, None, *out) == 0
+    torch.cuda.synchronize()
+    g2, h2, w2, l2 = _inputs(333, 64, 1500, torch.float32, 14)
+    idx, t = _entries(g2, 333, 1500, 5, l2)
+    layer2, out2 = dq.Vocab(h2, w2, k=5), _outputs(h2, w2)
+    ref2 = distill_ref(h2, w2, idx, t)
+    for seed in (20, 21):
+        _, hn, wn, ln = _inputs(400, 128, 2000, torch.bfloat16, seed)
+        ln[::3] = -1 if seed == 20 else 5
+        h.copy_(hn); w.copy_(wn); labels.copy_(ln)
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            assert dq.dq_distill_grad(layer2, idx, t, None, 1.0, None, *out2) == 0
+        torch.cuda.synchronize()
+        xent_ref(h, w, labels).check(*out, where="replay")
+        ref2.check(*out2, where="second stream")
+    need = dq.Vocab.workspace_bytes(h, w)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for n in (400, 1, 130, 400):                                             # fewer rows fit into the same workspace
+        small = dq.Vocab(h[:n], w, workspace=ws)
+        o = _outputs(h[:n], w)
+        assert dq.dq_xent_grad(small, labels[:n], None, *o) == 0
+        xent_ref(h[:n], w, labels[:n]).check(*o, where=n)
+
+
+def test_refusals_with_tensors(dq):
+    torch = _torch()
+    _, h, w, labels = _inputs(16, 32, 100, torch.float32, 15)
+    layer = dq.Vocab(h, w)
+    loss, lse, gh, gw = _outputs(h, w)
+    bad = dq.DQ_ERR_ARG
+    assert dq.dq_xent_grad(layer, labels.long(), None, loss, lse, gh, gw) == bad            # labels are int32
+    assert dq.dq_xent_grad(layer, labels[:8], None, loss, lse, gh, gw) == bad
+    assert dq.dq_xent_grad(layer, labels.cpu(), None, loss, lse, gh, gw) == bad
+    assert dq.dq_xent_grad(layer, labels, loss.double(), loss, lse, gh, gw) == bad
+    assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh.bfloat16(), gw) == bad
+    assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh, gw[:50]) == bad
+    assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh, torch.zeros(32, 100, device="cuda").t()) == bad
+    assert dq.dq_xent_loss(layer, labels, loss[:4], lse) == bad
+    assert dq.dq_distill_loss(layer, labels, loss, None, 1.0, loss, lse) == bad             # k = 0 holder
+    with pytest.raises(dq.DqError):
+        dq.Vocab(h.t().contiguous().t(), w)._bytes(dq.Vocab._shape(h.t().contiguous().t(), w, 0), True, w.device)
+    tiny = dq.Vocab(h, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert dq.dq_xent_grad(tiny, labels, None, loss, lse, gh, gw) == dq.DQ_ERR_SHAPE
+    only_loss = dq.Vocab(h, w, grad=False)
+    assert dq.dq_xent_grad(only_loss, labels, None, loss, lse, gh, gw) == dq.DQ_ERR_SHAPE
+    assert torch.isnan(loss).all() and torch.isnan(gh).all() and torch.isnan(gw).all()      # nothing was written
+
+
+@pytest.mark.parametrize("loss_kind", ["xent", "distill"])
+def test_gradients_against_differences(dq, loss_kind):
+    """Central differences of F = sum weight_n loss_n along random directions, F from the library's own losses.  With a step e
+    along a unit direction the difference quotient is off by F''' e^2 / 6 (third derivatives of a softmax loss along it: at
+    most 2 |x|^3 T^-1 sum weight) and by F's rounding over e; the bound below is evaluated, not guessed."""
+    torch = _torch()
+    n, d, V, T = 30, 24, 90, 1.0 if loss_kind == "xent" else 2.0
+    g, h, w, labels = _inputs(n, d, V, torch.float32, 16, scale=1.0)
+    idx, t = _entries(g, n, V, 4, labels)
+    weight = torch.rand(n, generator=g, device="cuda") + 0.5
+
+    def run(hh, ww):
+        if loss_kind == "xent":
+            return xent(dq, hh, ww, labels, weight), xent_ref(hh, ww, labels, weight)
+        return distill(dq, hh, ww, idx, t, None, T, weight), distill_ref(hh, ww, idx, t, None, T, weight)
+
+    (_, _, gh, gw), _ = run(h, w)
+    for which in (0, 1):
+        for rep in range(3):
+            u = torch.randn(h.shape if which == 0 else w.shape, generator=g, device="cuda")
+            u /= u.norm()
+            e = 2.0 ** -5
+            hi, lo = [(h + s * e * u, w) if which == 0 else (h, w + s * e * u) for s in (1, -1)]
+            (a, ra), (b, rb) = run(*hi), run(*lo)
+            quot = ((a[0].double() - b[0].double()) * weight.double()).sum().item() / (2 * e)
+            moved = hi[which].double() - lo[which].double()                             # the step that fp32 inputs really took
+            want = ((gh if which == 0 else gw).double() * moved).sum().item() / (2 * e)
+            # a row's logits move by at most r = max |u-row| |other row| per unit; |third derivative| of lse <= 2 (2r)^3
+            r = ((u @ w.t()) if which == 0 else (h @ u.t())).abs().max(1).values.double() / T
+            third = (weight.double() * T * T * 2 * (2 * r) ** 3).sum().item()
+            noise = ((ra.loss_err + rb.loss_err) * weight.double()).sum().item() / (2 * e)
+            gerr = 1e-5 * ((gh if which == 0 else gw).double().abs() * moved.abs()).sum().item() / (2 * e)
+            assert abs(quot - want) <= third * e * e / 6 + noise + gerr, (which, rep, quot, want)
+
+
+def test_loss_gradient_as_a_workers_message(dq):
+    """As it is used: M workers form the gradient of one output layer on their own rows, the codec quantises it and the
+    master steps.  The messages are bit-exact against the oracle's quantiser on the library's own gradients, and the next
+    round's losses are those of the stepped weights."""
+    torch = _torch()
+    import oracle
+    M, n, d, V, seed, eta, b, bx = 3, 50, 40, 120, 77, 0.5, 4, 8
+    _, _, w, _ = _inputs(1, d, V, torch.float32, 30)
+    rc, ctx = dq.dq_create(dq.make_config(V * d, M, b=b, bx=bx, seed=seed)); assert rc == 0
+    st = dq.State(w.flatten())
+    nb = dq.dq_packed_bytes(V * d, bx)
+    codes_x, delta_x = torch.zeros(nb, dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+    v = torch.zeros(M, V, d, device="cuda")
+    rows = [_inputs(n, d, V, torch.float32, 40 + i)[1:] for i in range(M)]
+    x = w.flatten().cpu().numpy()
+    zero = np.zeros(V * d, np.float32)
+    for rnd in range(3):
+        wt = st.x.view(V, d)
+        for i, (h, _, labels) in enumerate(rows):
+            layer = dq.Vocab(h, wt)
+            loss, lse, gh, _ = _outputs(h, wt)
+            if i < 2:
+                assert dq.dq_xent_grad(layer, labels, None, loss, lse, gh, v[i]) == 0
+                xent_ref(h, wt, labels).check(loss, lse, gh, v[i])
+            else:                                                            # this one learns from a teacher
+                idx, t = _entries(torch.Generator(device="cuda").manual_seed(rnd), n, V, 6, labels)
+                layer = dq.Vocab(h, wt, k=6)
+                assert dq.dq_distill_grad(layer, idx, t, None, 2.0, None, loss, lse, gh, v[i]) == 0
+                distill_ref(h, wt, idx, t, None, 2.0).check(loss, lse, gh, v[i])
+        grads = v.view(M, -1).cpu().numpy()
+        dq.ok(dq.dq_codec_round(ctx, v, st, rnd, eta, 0.0, codes_x, delta_x))
+        raw, delta = np.zeros((M, V * d), np.int32), np.zeros(M, np.float32)
+        for i in range(M):
+            raw[i], delta[i], _ = oracle.quantize(grads[i], b, seed, rnd, i, oracle.STREAM_GRAD)
+        oracle.master_step(raw, delta, zero, x, eta)
+        assert np.array_equal(st.x.cpu().numpy(), x)
+    dq.dq_destroy(ctx)
