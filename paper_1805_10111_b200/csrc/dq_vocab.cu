@@ -21,7 +21,8 @@ namespace {
 
 using namespace mma;
 
-enum { kLse = 0, kProb = 1, kGradH = 2, kGradW = 3 };     // what a product's epilogue does
+// What a product's epilogue does: (max, sum) of the logits; the same and the logits; the logits' gradient; the gradients.
+enum { kLse = 0, kProb = 1, kGradH = 2, kGradW = 3, kLogits = 4 };
 constexpr int kTileN = 256, kTileK = 64;
 constexpr int kMaxTop = DQ_VOCAB_MAX_TOP;
 constexpr int kHalf = kTileN / 2;                         // columns of an epilogue thread
@@ -34,17 +35,18 @@ struct Ctrl { int status; int count; };                   // head of the workspa
 // The workspace, carved from the caller's buffer (all parts 256-byte aligned).
 struct Work {
     Ctrl* ctrl;
-    int32_t *map, *inv, *tgt;      // compact row -> row, row -> compact row or -1, distillation: 0 / -1 has a target
+    int32_t *map, *tgt;            // compact row -> row; distillation: 0 or -1, whether a row has a target
     float4* rowc;                  // compact row: maximum in log2 units, factor of 2^(z - maximum), factor of q
     int32_t* eidx; float *eq, *elq, *emass;   // distillation: targets of a row by ascending class, q, log q, sum q
     float* zt;                     // logit at every target
     __nv_bfloat16* hp;             // [terms][n_pad][dp] compact rows of h
     __nv_bfloat16* wp;             // [terms][V][dp] w, where it cannot be read in place
+    float* z;                      // [n_pad][vc] the logits, where they are few enough to be kept (see run_loss)
     float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, log2 units
     __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
     float* dh;                     // [splits][n_pad][dq] sums of grad_h
     // sizes
-    int terms; int64_t n_pad, dp, dq, vc; int vtiles, parts, splits, kps; bool direct_w;
+    int terms; int64_t n_pad, dp, dq, vc; int vtiles, parts, splits, kps; bool direct_w, keep;
     int64_t bytes;
 };
 
@@ -68,7 +70,7 @@ Work carve(const dq_vocab* v, bool grad, int sms)
     char* base = static_cast<char*>(v->workspace);
     auto take = [&](int64_t bytes) { char* p = base + at; at = up(at + bytes, 256); return p; };
     w.ctrl = (Ctrl*)take(sizeof(Ctrl));
-    w.map = (int32_t*)take(4 * w.n_pad); w.inv = (int32_t*)take(4 * w.n_pad);
+    w.map = (int32_t*)take(4 * w.n_pad);
     w.rowc = (float4*)take(16 * w.n_pad);
     w.zt = (float*)take(4 * w.n_pad * k);
     if (v->k > 0) {
@@ -85,6 +87,8 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         const int64_t pieces = (v->V + vc - 1) / vc;                       // pieces of nearly the same size
         w.vc = up((v->V + pieces - 1) / pieces, kTileN);
         w.g = (__nv_bfloat16*)take(2 * w.terms * w.n_pad * w.vc);
+        w.keep = w.vc >= v->V && 4 * w.n_pad * w.vc <= kGradBytes;
+        if (w.keep) w.z = (float*)take(4 * w.n_pad * w.vc);
         // few rows: grad_h has fewer tiles than the GPU has SMs, so its sum over the vocabulary is split and joined
         const int cg = row_pairs(v->n), units = sms / cg;
         const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + kTileN - 1) / kTileN));
@@ -93,7 +97,7 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         if (splits > kit / 4) splits = kit / 4 > 0 ? kit / 4 : 1;
         w.kps = (kit + splits - 1) / splits;
         w.splits = (kit + w.kps - 1) / w.kps;
-        w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
+        if (w.splits > 1 || w.vc < v->V) w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
     }
     w.bytes = at;
     return w;
@@ -120,6 +124,11 @@ __device__ __forceinline__ void split_terms(float x, __nv_bfloat16 (&t)[TERMS])
 #pragma unroll
         for (int i = 1; i < TERMS; ++i) { t[i] = __float2bfloat16_rn(r); r -= __bfloat162float(t[i]); }
     }
+}
+
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 lo, __nv_bfloat16 hi)
+{
+    return (uint32_t)__bfloat16_as_ushort(lo) | ((uint32_t)__bfloat16_as_ushort(hi) << 16);
 }
 
 // One row of `d` values to its bf16 terms (pitch dp, zeros behind the row's end); a warp's work.
@@ -214,16 +223,17 @@ __global__ void __launch_bounds__(128) vocab_targets_kernel(const int32_t* __res
 }
 
 // Compact copy of the rows that have a target.  A block owns a range of rows; it counts the targets before its range (the list
-// is small and in L2) instead of waiting for a scan, then copies its own rows warp by warp.  Rows without a target get loss 0
-// and lse 0 here.  The last block writes the count and zeroes h's rows up to a whole tile of K (a zero of g times whatever the
+// is small and in L2) instead of waiting for a scan, then copies its own rows warp by warp.  Rows without a target get loss 0,
+// lse 0 and their zero row of grad_h here.  The last block writes the count and zeroes h's rows up to a whole tile of K (a zero of g times whatever the
 // buffer held would be NaN).
 template <bool F32>
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restrict__ h, int64_t ld, int d, const int32_t* __restrict__ tgt, int64_t V,
-                                                           int64_t n, int64_t rows_per_block, bool vec, float* loss, float* lse, Work w)
+                                                           int64_t n, int64_t rows_per_block, bool vec, float* loss, float* lse, void* gh,
+                                                           int64_t ld_gh, Work w)
 {
     pdl_prologue();
     __shared__ int s_sum[8];
-    __shared__ int s_rows[256];
+    __shared__ int s_rows[256], s_none[256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t r0 = blockIdx.x * rows_per_block, r1 = min(n, r0 + rows_per_block);
     int before = 0;
@@ -247,11 +257,20 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
         for (int i = 0; i < 8; ++i) { if (i < warp) off += s_sum[i]; total += s_sum[i]; }
         off += __popc(bal & ((1u << lane) - 1u));
         if (mine < r1) {
-            w.inv[mine] = has ? before + off : -1;
             if (has) { w.map[before + off] = (int32_t)mine; s_rows[off] = threadIdx.x; }
-            else { loss[mine] = 0.0f; if (lse) lse[mine] = 0.0f; }
+            else { s_none[threadIdx.x - off] = threadIdx.x; loss[mine] = 0.0f; if (lse) lse[mine] = 0.0f; }
         }
         __syncthreads();
+        if (gh) {
+            const int none = (int)min((int64_t)256, r1 - r) - total;
+            for (int i = warp; i < none; i += 8) {
+                const int64_t at = (r + s_none[i]) * ld_gh;
+                for (int j = lane; j < d; j += 32) {
+                    if (F32) static_cast<float*>(gh)[at + j] = 0.0f;
+                    else static_cast<__nv_bfloat16*>(gh)[at + j] = __float2bfloat16_rn(0.0f);
+                }
+            }
+        }
         for (int i = warp; i < total; i += 8)
             copy_row<F32>(h, (r + s_rows[i]) * ld, d, vec, w.hp + (int64_t)(before + i) * w.dp, w.n_pad * w.dp, (int)w.dp, lane);
         before += total;
@@ -327,21 +346,135 @@ __global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const in
     }
 }
 
-// grad_h = the splits' sums, rounded once; rows without a target get zeros.  A warp per row.
+// The row's (max, sum) pairs joined, by a whole block of 256 threads; every thread gets them.
+__device__ __forceinline__ float2 block_join(const float2* p, int parts)
+{
+    __shared__ float2 s_part[8];
+    float m = -INFINITY, s = 0.0f;
+    for (int t = threadIdx.x; t < parts; t += 256) {
+        const float2 q = p[t];
+        const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
+        s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
+        m = nm;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float qm = __shfl_xor_sync(0xFFFFFFFFu, m, o), qs = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        const float nm = fmaxf(m, qm), use = nm == -INFINITY ? 0.0f : nm;
+        s = s * exp2f(m - use) + qs * exp2f(qm - use);
+        m = nm;
+    }
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = make_float2(m, s);
+    __syncthreads();
+    m = -INFINITY; s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 q = s_part[i];
+        const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
+        s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
+        m = nm;
+    }
+    return make_float2(m, s);
+}
+
+// Kept logits to their gradient: a block takes 2048 columns of a row (and joins the row's pairs itself: a few KB from L2 against
+// a launch).  Column block 0 also writes the loss.  Rows behind the last one, up to a whole tile of K, and columns behind the
+// vocabulary are zeros: the gradients' products read them.
+constexpr int kRowCols = 2048;
 template <bool F32>
-__global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int64_t n, int d, float scale, void* __restrict__ out, int64_t ld)
+__global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int64_t V, int k, int blocks_per_row, const int32_t* __restrict__ labels,
+                                                         const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+                                                         float* __restrict__ lse)
 {
     pdl_prologue();
-    const int lane = threadIdx.x & 31;
-    const float alpha = scale != 0.0f ? scale / (float)max(w.ctrl->count, 1) : 1.0f;
-    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < n; r += (int64_t)gridDim.x * 8) {
-        const int i = w.inv[r];
-        for (int j = lane; j < d; j += 32) {
-            float s = 0.0f;
-            if (i >= 0) for (int q = 0; q < w.splits; ++q) s += w.dh[((int64_t)q * w.n_pad + i) * w.dq + j];
-            s *= alpha;
-            if (F32) static_cast<float*>(out)[r * ld + j] = s;
-            else static_cast<__nv_bfloat16*>(out)[r * ld + j] = __float2bfloat16_rn(s);
+    constexpr int TERMS = F32 ? 3 : 1;
+    const int count = w.ctrl->count, i = blockIdx.x / blocks_per_row, cb = blockIdx.x % blocks_per_row;
+    if (i >= (count + kTileK - 1) / kTileK * kTileK) return;
+    const int64_t plane = w.n_pad * w.vc;
+    __nv_bfloat16* g = w.g + (int64_t)i * w.vc;
+    const int64_t col = (int64_t)cb * kRowCols + threadIdx.x * 8;
+    float f[8];
+    float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int64_t row = 0;
+    const float* z = w.z + (int64_t)i * w.vc;
+    if (i < count) {
+        if (col < w.vc) load8_rw(z + col, f);
+        row = w.map[i];
+        const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts);
+        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
+        const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f;
+        rc = make_float4(ms.x, wt * mass / ms.y, wt, 0.0f);
+        if (cb == 0 && threadIdx.x < 32) {
+            double sum = 0.0;
+            if (k == 0) {
+                sum = l - (double)z[labels[row]];
+            } else {
+                for (int j = threadIdx.x; j < k; j += 32) {
+                    const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
+                    if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                sum *= (double)temp * (double)temp;
+            }
+            if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
+        }
+    }
+    if (col < w.vc) {
+        uint32_t e[TERMS][4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            __nv_bfloat16 t[TERMS], u[TERMS];
+#pragma unroll
+            for (int x = j; x < j + 2; ++x) f[x] = (i < count && col + x < V) ? rc.y * ex2(__fmaf_rn(f[x], c2, -rc.x)) : 0.0f;
+            split_terms<TERMS>(f[j], t); split_terms<TERMS>(f[j + 1], u);
+#pragma unroll
+            for (int p = 0; p < TERMS; ++p) e[p][j / 2] = pack2(t[p], u[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < TERMS; ++p) *reinterpret_cast<uint4*>(g + p * plane + col) = make_uint4(e[p][0], e[p][1], e[p][2], e[p][3]);
+    }
+    if (i >= count) return;
+    __syncthreads();                                       // the targets' entries are written over what the threads above wrote
+    const int64_t lo = (int64_t)cb * kRowCols, hi = lo + kRowCols;
+    for (int j = threadIdx.x; j < (k > 0 ? k : 1); j += 256) {
+        const int32_t at = k > 0 ? w.eidx[row * k + j] : labels[row];
+        if (at == INT32_MAX || at < lo || at >= hi || (j > 0 && w.eidx[row * k + j - 1] == at)) continue;
+        float x = rc.y * ex2(__fmaf_rn(z[at], c2, -rc.x));
+        if (k == 0) x -= rc.z;
+        else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * rc.z;
+        __nv_bfloat16 t[TERMS];
+        split_terms<TERMS>(x, t);
+#pragma unroll
+        for (int p = 0; p < TERMS; ++p) g[p * plane + at] = t[p];
+    }
+}
+
+// grad_h = the splits' sums in a fixed order, rounded once.  A thread takes four columns of a row.
+template <bool F32>
+__global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int d, float scale, void* __restrict__ out, int64_t ld)
+{
+    pdl_prologue();
+    const int count = w.ctrl->count, per_row = (d + 3) / 4;
+    const float alpha = scale != 0.0f ? scale / (float)max(count, 1) : 1.0f;
+    const int64_t plane = w.n_pad * w.dq;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < (int64_t)count * per_row; t += (int64_t)gridDim.x * 256) {
+        const int64_t i = t / per_row; const int j = (int)(t % per_row) * 4;
+        const float* p = w.dh + i * w.dq + j;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+        for (int q = 0; q < w.splits; ++q) {
+            const float4 x = *reinterpret_cast<const float4*>(p + q * plane);
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        const float v[4] = {s.x * alpha, s.y * alpha, s.z * alpha, s.w * alpha};
+        const int64_t at = (int64_t)w.map[i] * ld + j;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (j + c < d) {
+                if (F32) static_cast<float*>(out)[at + c] = v[c];
+                else static_cast<__nv_bfloat16*>(out)[at + c] = __float2bfloat16_rn(v[c]);
+            }
         }
     }
 }
@@ -357,11 +490,11 @@ struct MmaArgs {
     int v0;                  // first class of the piece
     int k;                   // targets per row (0: one label)
     float c2;                // log2(e) / T
-    float scale;             // kGradW: not 0: the result times scale / (rows with a target)
-    int first;               // kGradH: first piece of the vocabulary
-    int align;               // kGradW: rows of the output start on 16 bytes (1), 32 (2) or neither (0)
+    float scale;             // gradients: not 0: the result times scale / (rows with a target)
+    int first, last;         // kGradH: first piece of the vocabulary; the sum is complete and goes to the output
+    int align;               // gradients: rows of the output start on 16 bytes (1), 32 (2) or neither (0)
     const int32_t* eidx;     // targets' classes [n][max(k, 1)], ascending
-    void* out; int64_t ld;   // kGradW
+    void* out; int64_t ld;   // gradients
 };
 
 // Products of bf16 terms for fp32 operands, smallest first so that the leading one is rounded least: (2,0) (0,2) (1,1) (1,0)
@@ -387,11 +520,6 @@ __device__ __forceinline__ Tile decode(int t, int mt, int nt, int kit, int kps, 
     r.k0 = split_k ? r.split * kps : 0;
     r.k1 = split_k ? min(kit, r.k0 + kps) : kit;
     return r;
-}
-
-__device__ __forceinline__ uint32_t pack2(__nv_bfloat16 lo, __nv_bfloat16 hi)
-{
-    return (uint32_t)__bfloat16_as_ushort(lo) | ((uint32_t)__bfloat16_as_ushort(hi) << 16);
 }
 
 // 32 bytes to one 32-byte sector, or as two stores where the row only starts on 16 bytes.
@@ -551,7 +679,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         float* const stage = staging + (warp - 4) * kPiece * 32 + lane;       // [column][lane]
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const float alpha = (KIND == kGradW && a.scale != 0.0f) ? a.scale / (float)max(count, 1) : 1.0f;
+        const float alpha = a.scale != 0.0f ? a.scale / (float)max(count, 1) : 1.0f;
         int acc = 0; uint32_t aph = 0; bool ok = true;
         for (int t = first; t < tiles && ok; t += step) {
             const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
@@ -561,7 +689,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             // targets of the row: the first one not before the half tile
             int64_t e0 = 0; int pos = 0, next = INT32_MAX; const int ke = a.k > 0 ? a.k : 1, v_at = a.v0 + col;
             float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if ((KIND == kLse || KIND == kProb) && r < count) {
+            if ((KIND == kLse || KIND == kProb) && r < count) {       // (kept logits: the rows' kernel looks them up itself)
                 e0 = (int64_t)w.map[r] * ke;
                 int lo = 0, hi = ke;
                 while (lo < hi) { const int mid = (lo + hi) >> 1; if (a.eidx[e0 + mid] < v_at) lo = mid + 1; else hi = mid; }
@@ -574,6 +702,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             for (int j = 0; j < kHalf; ++j) f[j] = 0.0f;
             const int steps = (q.k1 - q.k0) * a.pairs;
             for (int i0 = 0; i0 < steps; i0 += kSegment) {
+                __syncwarp();
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(tfull(acc), aph, gave_up))) { ok = false; break; }    // the warp leaves as one
                 fence_after_sync();
                 const uint32_t d = tmem + lanes + acc * kTileN + half * kHalf;
@@ -592,10 +721,18 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             }
             if (!ok) break;
 
-            if (KIND == kLse) {
+            if (KIND == kLse || KIND == kLogits) {
 #pragma unroll
                 for (int c = 0; c < kHalf; c += kPiece) {
-                    if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
+                    if (KIND == kLogits) {
+                        if (r < count && c < have) {
+                            float* o = w.z + (int64_t)r * w.vc + col + c;
+                            float x[8], y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) { x[j] = f[c + j]; y[j] = f[c + 8 + j]; }
+                            store8(o, x); store8(o + 8, y);
+                        }
+                    } else if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
 #pragma unroll
                         for (int j = 0; j < kPiece; ++j) stage[j * 32] = f[c + j];
                         while (next < v_at + c + kPiece) {
@@ -638,27 +775,34 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                     }
                     store_terms<F32 ? 3 : 1>(o + c, w.n_pad * w.vc, f + c, true);
                 }
-            } else if (KIND == kGradH) {
-                if (r < count) {
+            } else if (r < mdim) {
+                if (KIND == kGradH && !a.first) {
+                    const float* o = w.dh + ((int64_t)q.split * w.n_pad + r) * w.dq + col;
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += 8) {
+                        if (col + c < w.dq) {
+                            float y[8];
+                            load8_rw(o + c, y);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) f[c + j] += y[j];
+                        }
+                    }
+                }
+                if (KIND == kGradH && !a.last) {
                     float* o = w.dh + ((int64_t)q.split * w.n_pad + r) * w.dq + col;
 #pragma unroll
                     for (int c = 0; c < kHalf; c += 8) {
                         if (col + c < w.dq) {
-                            float x[8], y[8];
+                            float x[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) x[j] = f[c + j];
-                            if (!a.first) {
-                                load8_rw(o + c, y);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) x[j] += y[j];
-                            }
                             store8(o + c, x);
                         }
                     }
+                    continue;
                 }
-            } else if (r < mdim) {
-                const int64_t at = (int64_t)(a.v0 + r) * a.ld + col;
-                if (KIND == kGradW && alpha != 1.0f) {
+                const int64_t at = (int64_t)(KIND == kGradH ? w.map[r] : a.v0 + r) * a.ld + col;
+                if (alpha != 1.0f) {
 #pragma unroll
                     for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
                 }
@@ -768,6 +912,12 @@ bool launch_mma(int64_t m, int64_t nt, const CUtensorMap& ma, const CUtensorMap&
 struct Targets { const int32_t* labels; const int32_t* top_idx; const float* top_logits; const float* teacher_lse; float temp; };
 struct Grads { const float* weight; void* gh; int64_t ld_h; void* gw; int64_t ld_w; };
 
+int row_alignment(const void* p, int64_t row_bytes)
+{
+    if (!ptr_aligned(p, 16) || row_bytes % 16) return 0;
+    return ptr_aligned(p, 32) && row_bytes % 32 == 0 ? 2 : 1;
+}
+
 template <bool F32>
 int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
 {
@@ -781,7 +931,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
                             1.0f / t.temp, n, k, V, w) == cudaSuccess;
     const int64_t gblocks = min((int64_t)dev.sms * 2, (n + 7) / 8), per = (n + gblocks - 1) / gblocks;
     ok = ok && launch_k(vocab_gather_kernel<F32>, dim3((unsigned)((n + per - 1) / per)), dim3(256), 0, st, v->h, v->ld_h, d, k > 0 ? w.tgt : t.labels,
-                        V, n, per, ptr_aligned(v->h, 16) && v->ld_h * elem % 16 == 0, loss, lse, w) == cudaSuccess;
+                        V, n, per, ptr_aligned(v->h, 16) && v->ld_h * elem % 16 == 0, loss, lse, g ? g->gh : nullptr, g ? g->ld_h : 0, w) == cudaSuccess;
     if (!w.direct_w)
         ok = ok && launch_k(vocab_weights_kernel<F32>, grid8(V), dim3(256), 0, st, v->w, v->ld_w, d, V, ptr_aligned(v->w, 16) && v->ld_w * elem % 16 == 0, w) == cudaSuccess;
     const __nv_bfloat16* wsrc = w.direct_w ? static_cast<const __nv_bfloat16*>(v->w) : w.wp;
@@ -795,8 +945,18 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     ok = ok && make_map(&mw, wsrc, d, V, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wsrc, d, V, wpitch, T, V * wpitch, kTileN / 2);
     if (!ok) return DQ_ERR_CUDA;
     a.cols = (int)V; a.kdim = d;
-    ok = launch_mma<kLse, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
-    ok = ok && launch_k(vocab_join_kernel, grid8(n), dim3(256), 0, st, w, k, t.labels, g ? g->weight : (const float*)nullptr, t.temp, a.c2, loss, lse) == cudaSuccess;
+    const float* weight = g ? g->weight : nullptr;
+    if (w.keep) {
+        // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
+        // cheaper than forming them again (2 d flops, six times that for fp32) and merges the join with what follows it.
+        ok = launch_mma<kLogits, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
+        const int per_row = (int)((w.vc + kRowCols - 1) / kRowCols);
+        ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(up(n, kTileK) * per_row)), dim3(256), 0, st, w, V, k, per_row, t.labels, weight, t.temp, a.c2,
+                            loss, lse) == cudaSuccess;
+    } else {
+        ok = launch_mma<kLse, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
+        ok = ok && launch_k(vocab_join_kernel, grid8(n), dim3(256), 0, st, w, k, t.labels, weight, t.temp, a.c2, loss, lse) == cudaSuccess;
+    }
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
 
     CUtensorMap mg_k, mg_mn, mw_mn, mh_mn;
@@ -810,14 +970,18 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         ok = make_map(&mw, wv, d, vn, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wv, d, vn, wpitch, T, V * wpitch, kTileN / 2) &&
              make_map(&mw_mn, wv, d, vn, wpitch, T, V * wpitch, kTileK);
         a.v0 = (int)v0; a.cols = vn; a.kdim = d; a.splits = 1;
-        ok = ok && launch_mma<kProb, F32>(n, (vn + kTileN - 1) / kTileN, mh, mw, mw2, a, w, dev.sms, st);
-        a.cols = d; a.mdim = vn; a.out = g->gw; a.ld = g->ld_w; a.align = !ptr_aligned(g->gw, 16) || g->ld_w * elem % 16 ? 0 : !ptr_aligned(g->gw, 32) || g->ld_w * elem % 32 ? 1 : 2;
+        if (!w.keep) ok = ok && launch_mma<kProb, F32>(n, (vn + kTileN - 1) / kTileN, mh, mw, mw2, a, w, dev.sms, st);
+        a.cols = d; a.mdim = vn; a.out = g->gw; a.ld = g->ld_w; a.align = row_alignment(g->gw, g->ld_w * elem);
         ok = ok && launch_mma<kGradW, F32>(vn, ntd, mg_mn, mh_mn, mh_mn, a, w, dev.sms, st);
-        a.kdim = vn; a.kps = w.kps; a.first = v0 == 0;
+        a.kdim = vn; a.kps = w.kps; a.first = v0 == 0; a.last = w.splits == 1 && v0 + w.vc >= V;
+        a.out = g->gh; a.ld = g->ld_h; a.align = row_alignment(g->gh, g->ld_h * elem);
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
         ok = ok && launch_mma<kGradH, F32>(n, (int64_t)ntd * a.splits, mg_k, mw_mn, mw_mn, a, w, dev.sms, st);
     }
-    ok = ok && launch_k(vocab_grad_h_kernel<F32>, grid8(n), dim3(256), 0, st, w, n, d, a.scale, g->gh, g->ld_h) == cudaSuccess;
+    if (w.splits > 1) {
+        const int64_t need = (n * ((d + 3) / 4) + 255) / 256;
+        ok = ok && launch_k(vocab_grad_h_kernel<F32>, dim3((unsigned)min((int64_t)blocks, need)), dim3(256), 0, st, w, d, a.scale, g->gh, g->ld_h) == cudaSuccess;
+    }
     return ok ? DQ_OK : DQ_ERR_CUDA;
 }
 
