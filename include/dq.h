@@ -299,8 +299,8 @@ typedef struct {
     void* workspace; int64_t workspace_bytes;   /* 256-byte aligned, at least dq_vocab_workspace_bytes      */
 } dq_vocab;
 
-/* Bytes that the calls on these shapes need (grad = 0: the losses alone); -1 for sizes out of range.  Looks at format, k,
- * n, d, V, w and ld_w only; asks the current device for its number of SMs. */
+/* Bytes that the calls need (grad = 0: the losses alone) on these shapes and on fewer rows; -1 for sizes out of range.  Looks
+ * at format, k, n, d, V, w and ld_w only; asks the current device for its number of SMs. */
 int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad);
 
 /* loss [n]; lse [n] or NULL; labels [n]. */

@@ -180,14 +180,14 @@ class Msgs:
 
 class Vocab:
     """Hidden states h [n, d], weights w [V, d] of a large output layer, a workspace for the losses over them (with their
-    gradients unless grad=False) and the dq_vocab view.  Rows may be strided (the last dimension is contiguous).  k: the
+    gradients unless grad=False, which the gradient calls then refuse) and the dq_vocab view.  Rows may be strided (the last dimension is contiguous).  k: the
     teacher's entries per row for the distillation calls, 0 for cross-entropy.  `workspace`: a uint8 tensor to use
     instead of a new one, of at least workspace_bytes(h, w, k, grad) bytes; it serves one call at a time."""
 
     def __init__(self, h, w, k=0, grad=True, workspace=None):
         import torch
-        self.h, self.w, self.device = h, w, w.device
-        self.grad = bool(grad)
+        self.h, self.w, self.device, self.index = h, w, w.device, w.get_device()
+        self.f32, self.i32, self.cuda, self.grad = torch.float32, torch.int32, torch.cuda, bool(grad)
         self.c = self._shape(h, w, k)
         self.n, self.d, self.V, self.k = self.c.n, self.c.d, self.c.V, self.c.k
         if h.device != w.device:
@@ -359,26 +359,25 @@ def dq_quantize_pack_static(v, d, M, b, seed, round_, codes, stride, scale, stre
                                          _ptr(scale), _stream(stream))
 
 
-def _bad(layer, tensors, rows, types, sizes):
-    """Whether a tensor of a vocabulary call is not what the library will take it for (None stands for an absent one)."""
-    for t, dt, size in zip(tensors, types, sizes):
-        if t is not None and (str(t.dtype) != dt or t.device != layer.device or not t.is_contiguous() or t.numel() != size):
+def _bad(layer, tensors, grads=()):
+    """Whether a tensor of a vocabulary call is not what the library will take it for.  tensors: (tensor or None, dtype,
+    number of values) of the dense ones; grads: (tensor, the input whose shape it has)."""
+    index = layer.index
+    for t, dtype, size in tensors:
+        if t is not None and (t.dtype is not dtype or t.get_device() != index or t.numel() != size or not t.is_contiguous()):
             return True
-    for t, like in rows:
-        if t is None or t.dtype != like.dtype or t.device != layer.device or t.shape != like.shape or _pitch(t) < 0:
+    for t, like in grads:
+        if t is None or t.dtype is not like.dtype or t.get_device() != index or t.shape != like.shape or _pitch(t) < 0:
             return True
     return False
 
 
 def _vocab_call(fn, layer, args, stream):
-    import torch
-    if torch.cuda.current_device() == layer.device.index:
-        return fn(layer.ref, *args, _stream(stream))
-    with torch.cuda.device(layer.device):
-        return fn(layer.ref, *args, _stream(stream))
-
-
-_F, _I = "torch.float32", "torch.int32"
+    cuda = layer.cuda
+    if cuda.current_device() == layer.index:
+        return fn(layer.ref, *args, cuda.current_stream().cuda_stream if stream is None else stream)
+    with cuda.device(layer.index):
+        return fn(layer.ref, *args, cuda.current_stream().cuda_stream if stream is None else stream)
 
 
 def dq_vocab_workspace_bytes(layer: Vocab, grad=True):
@@ -386,30 +385,36 @@ def dq_vocab_workspace_bytes(layer: Vocab, grad=True):
 
 
 def dq_xent_loss(layer: Vocab, labels, loss, lse=None, stream=None):
-    if _bad(layer, (labels, loss, lse), (), (_I, _F, _F), (layer.n,) * 3):
+    n, f32 = layer.n, layer.f32
+    if _bad(layer, ((labels, layer.i32, n), (loss, f32, n), (lse, f32, n))):
         return DQ_ERR_ARG
     return _vocab_call(lib().dq_xent_loss, layer, (_ptr(labels), _ptr(loss), _ptr(lse)), stream)
 
 
 def dq_xent_grad(layer: Vocab, labels, weight, loss, lse, grad_h, grad_w, stream=None):
-    if _bad(layer, (labels, weight, loss, lse), ((grad_h, layer.h), (grad_w, layer.w)), (_I, _F, _F, _F), (layer.n,) * 4):
+    if not layer.grad:
+        return DQ_ERR_SHAPE
+    n, f32 = layer.n, layer.f32
+    if _bad(layer, ((labels, layer.i32, n), (weight, f32, n), (loss, f32, n), (lse, f32, n)), ((grad_h, layer.h), (grad_w, layer.w))):
         return DQ_ERR_ARG
     return _vocab_call(lib().dq_xent_grad, layer, (_ptr(labels), _ptr(weight), _ptr(loss), _ptr(lse), _ptr(grad_h), _pitch(grad_h),
                                                    _ptr(grad_w), _pitch(grad_w)), stream)
 
 
 def dq_distill_loss(layer: Vocab, top_idx, top_logits, teacher_lse, temperature, loss, lse=None, stream=None):
-    n, k = layer.n, layer.k
-    if _bad(layer, (top_idx, top_logits, teacher_lse, loss, lse), (), (_I, _F, _F, _F, _F), (n * k, n * k, n, n, n)):
+    n, nk, f32 = layer.n, layer.n * layer.k, layer.f32
+    if _bad(layer, ((top_idx, layer.i32, nk), (top_logits, f32, nk), (teacher_lse, f32, n), (loss, f32, n), (lse, f32, n))):
         return DQ_ERR_ARG
     return _vocab_call(lib().dq_distill_loss, layer, (_ptr(top_idx), _ptr(top_logits), _ptr(teacher_lse), float(temperature), _ptr(loss),
                                                       _ptr(lse)), stream)
 
 
 def dq_distill_grad(layer: Vocab, top_idx, top_logits, teacher_lse, temperature, weight, loss, lse, grad_h, grad_w, stream=None):
-    n, k = layer.n, layer.k
-    if _bad(layer, (top_idx, top_logits, teacher_lse, weight, loss, lse), ((grad_h, layer.h), (grad_w, layer.w)),
-            (_I, _F, _F, _F, _F, _F), (n * k, n * k, n, n, n, n)):
+    if not layer.grad:
+        return DQ_ERR_SHAPE
+    n, nk, f32 = layer.n, layer.n * layer.k, layer.f32
+    if _bad(layer, ((top_idx, layer.i32, nk), (top_logits, f32, nk), (teacher_lse, f32, n), (weight, f32, n), (loss, f32, n), (lse, f32, n)),
+            ((grad_h, layer.h), (grad_w, layer.w))):
         return DQ_ERR_ARG
     return _vocab_call(lib().dq_distill_grad, layer, (_ptr(top_idx), _ptr(top_logits), _ptr(teacher_lse), float(temperature), _ptr(weight),
                                                       _ptr(loss), _ptr(lse), _ptr(grad_h), _pitch(grad_h), _ptr(grad_w), _pitch(grad_w)), stream)

@@ -11,6 +11,7 @@
 // turned into g (rounded to bf16) in the kernel's epilogue, and two more products read the piece while it is warm.
 // Every sum has a fixed order: equal inputs give equal bytes.
 #include <math.h>
+#include <atomic>
 #include <cuda_bf16.h>
 
 #include "dq_common.cuh"
@@ -21,8 +22,8 @@ namespace {
 
 using namespace mma;
 
-// What a product's epilogue does: (max, sum) of the logits; the same and the logits; the logits' gradient; the gradients.
-enum { kLse = 0, kProb = 1, kGradH = 2, kGradW = 3, kLogits = 4 };
+// What a product's epilogue does: (max, sum) of the logits; the same and the logits; the logits' gradient; both gradients.
+enum { kLse = 0, kLogits = 1, kProb = 2, kGrads = 3 };
 constexpr int kTileN = 256, kTileK = 64;
 constexpr int kMaxTop = DQ_VOCAB_MAX_TOP;
 constexpr int kHalf = kTileN / 2;                         // columns of an epilogue thread
@@ -94,7 +95,10 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + kTileN - 1) / kTileN));
         const int kit = (int)(w.vc / kTileK);
         int splits = tiles < 1 || tiles >= units ? 1 : units / tiles;
-        if (splits > kit / 4) splits = kit / 4 > 0 ? kit / 4 : 1;
+        // at least 512 classes to a split (256 for fp32, which takes six products of each): below that the shares' traffic outweighs
+        // the products (64 x 512 x 2000 fp32: 44 us at 256, 50 at 512, 63 at 1024; bf16 26, 27, 28)
+        const int least = f32 ? 4 : 8;
+        if (splits > kit / least) splits = kit / least > 0 ? kit / least : 1;
         w.kps = (kit + splits - 1) / splits;
         w.splits = (kit + w.kps - 1) / w.kps;
         if (w.splits > 1 || w.vc < v->V) w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
@@ -131,58 +135,72 @@ __device__ __forceinline__ uint32_t pack2(__nv_bfloat16 lo, __nv_bfloat16 hi)
     return (uint32_t)__bfloat16_as_ushort(lo) | ((uint32_t)__bfloat16_as_ushort(hi) << 16);
 }
 
-// One row of `d` values to its bf16 terms (pitch dp, zeros behind the row's end); a warp's work.
+// Values j..j+7 of a row of `d` to their bf16 terms, zeros behind the row's end.
 template <bool F32>
-__device__ __forceinline__ void copy_row(const void* src, int64_t off, int d, bool vec, __nv_bfloat16* dst, int64_t plane, int dp, int lane)
+__device__ __forceinline__ void copy8(const void* src, int64_t off, int j, int d, bool vec, __nv_bfloat16* dst, int64_t plane)
 {
     if (!F32) {
-        const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(src) + off;
-        for (int j = lane * 8; j < dp; j += 256) {
-            uint4 q;
-            if (vec && j + 8 <= d) {
-                q = __ldg(reinterpret_cast<const uint4*>(s + j));
-            } else {
-                __nv_bfloat16 e[8];
+        const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(src) + off + j;
+        uint4 q;
+        if (vec && j + 8 <= d) {
+            q = __ldg(reinterpret_cast<const uint4*>(s));
+        } else {
+            __nv_bfloat16 e[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = j + i < d ? s[j + i] : __float2bfloat16_rn(0.0f);
-                q = *reinterpret_cast<uint4*>(e);
-            }
-            *reinterpret_cast<uint4*>(dst + j) = q;
+            for (int i = 0; i < 8; ++i) e[i] = j + i < d ? s[i] : __float2bfloat16_rn(0.0f);
+            q = make_uint4(pack2(e[0], e[1]), pack2(e[2], e[3]), pack2(e[4], e[5]), pack2(e[6], e[7]));
         }
+        *reinterpret_cast<uint4*>(dst) = q;
     } else {
-        const float* s = static_cast<const float*>(src) + off;
-        for (int j = lane * 8; j < dp; j += 256) {
-            float x[8];
-            if (vec && j + 8 <= d) {
-                const float4 a = __ldg(reinterpret_cast<const float4*>(s + j)), b = __ldg(reinterpret_cast<const float4*>(s + j + 4));
-                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-            } else {
+        const float* s = static_cast<const float*>(src) + off + j;
+        float x[8];
+        if (vec && j + 8 <= d) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(s)), b = __ldg(reinterpret_cast<const float4*>(s + 4));
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = j + i < d ? s[j + i] : 0.0f;
-            }
-            __nv_bfloat16 e[3][8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                __nv_bfloat16 t[3];
-                split_terms<3>(x[i], t);
-                e[0][i] = t[0]; e[1][i] = t[1]; e[2][i] = t[2];
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(dst + p * plane + j) = *reinterpret_cast<uint4*>(e[p]);
+            for (int i = 0; i < 8; ++i) x[i] = j + i < d ? s[i] : 0.0f;
         }
+        uint32_t e[3][4];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            __nv_bfloat16 t[3], u[3];
+            split_terms<3>(x[i], t); split_terms<3>(x[i + 1], u);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) e[p][i / 2] = pack2(t[p], u[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(dst + p * plane) = make_uint4(e[p][0], e[p][1], e[p][2], e[p][3]);
+    }
+}
+
+// w where tensor maps cannot read it in place (fp32, or rows that do not start on 16 bytes): its bf16 terms, rows padded.  Done by the
+// blocks from `first` on of whichever kernel starts the call.
+struct Weights { const void* src; int64_t ld, V; int d, vec, first; };
+template <bool F32>
+__device__ __forceinline__ void copy_weights(const Weights& q, const Work& w)
+{
+    const int per = (int)(w.dp / 8);
+    const int64_t total = q.V * per, step = (int64_t)(gridDim.x - q.first) * 256;
+#pragma unroll 4
+    for (int64_t t = (int64_t)(blockIdx.x - q.first) * 256 + threadIdx.x; t < total; t += step) {
+        const int64_t r = t / per; const int j = (int)(t - r * per) * 8;
+        copy8<F32>(q.src, r * q.ld, j, q.d, q.vec, w.wp + r * w.dp + j, q.V * w.dp);
     }
 }
 
 // Targets of the distillation loss: a warp takes a row, orders its present entries by class (ties by place in the list; the
 // epilogues walk them in step with the columns) and forms q.  Absent entries (class outside 0..V-1, logit -inf) go to the end
 // with q = 0.  The rank of an entry is the number of entries before it: K^2 comparisons, K <= 256.
-__global__ void __launch_bounds__(128) vocab_targets_kernel(const int32_t* __restrict__ idx, const float* __restrict__ logits,
-                                                            const float* __restrict__ teacher_lse, float inv_t, int64_t n, int k, int64_t V, Work w)
+template <bool F32>
+__global__ void __launch_bounds__(256) vocab_targets_kernel(const int32_t* __restrict__ idx, const float* __restrict__ logits,
+                                                            const float* __restrict__ teacher_lse, float inv_t, int64_t n, int k, int64_t V, Weights q, Work w)
 {
     pdl_prologue();
-    __shared__ int32_t s_idx[4][kMaxTop];
+    if (blockIdx.x >= q.first) { copy_weights<F32>(q, w); return; }
+    __shared__ int32_t s_idx[8][kMaxTop];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + warp; row < n; row += (int64_t)gridDim.x * 4) {
+    for (int64_t row = (int64_t)blockIdx.x * 8 + warp; row < n; row += (int64_t)q.first * 8) {
         const int32_t* ri = idx + row * k; const float* rt = logits + row * k;
         float m = -INFINITY; bool any = false;
         for (int j = lane; j < k; j += 32) {
@@ -210,10 +228,10 @@ __global__ void __launch_bounds__(128) vocab_targets_kernel(const int32_t* __res
             const int32_t i = s_idx[warp][j];
             int rank = 0;
             for (int o = 0; o < k; ++o) { const int32_t x = s_idx[warp][o]; rank += x < i || (x == i && o < j); }
-            float lq = 0.0f, q = 0.0f;
-            if (i != INT32_MAX) { lq = rt[j] * inv_t - tl; q = expf(lq); }
-            mass += q;
-            w.eidx[row * k + rank] = i; w.eq[row * k + rank] = q; w.elq[row * k + rank] = lq;
+            float lq = 0.0f, p = 0.0f;
+            if (i != INT32_MAX) { lq = rt[j] * inv_t - tl; p = expf(lq); }
+            mass += p;
+            w.eidx[row * k + rank] = i; w.eq[row * k + rank] = p; w.elq[row * k + rank] = lq;
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xFFFFFFFFu, mass, o);
@@ -229,9 +247,10 @@ __global__ void __launch_bounds__(128) vocab_targets_kernel(const int32_t* __res
 template <bool F32>
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restrict__ h, int64_t ld, int d, const int32_t* __restrict__ tgt, int64_t V,
                                                            int64_t n, int64_t rows_per_block, bool vec, float* loss, float* lse, void* gh,
-                                                           int64_t ld_gh, Work w)
+                                                           int64_t ld_gh, Weights q, Work w)
 {
     pdl_prologue();
+    if (blockIdx.x >= q.first) { copy_weights<F32>(q, w); return; }
     __shared__ int s_sum[8];
     __shared__ int s_rows[256], s_none[256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -271,11 +290,15 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
                 }
             }
         }
-        for (int i = warp; i < total; i += 8)
-            copy_row<F32>(h, (r + s_rows[i]) * ld, d, vec, w.hp + (int64_t)(before + i) * w.dp, w.n_pad * w.dp, (int)w.dp, lane);
+        const int per = (int)(w.dp / 8);
+#pragma unroll 4
+        for (int t = threadIdx.x; t < total * per; t += 256) {
+            const int i = t / per, j = (t - i * per) * 8;
+            copy8<F32>(h, (r + s_rows[i]) * ld, j, d, vec, w.hp + (int64_t)(before + i) * w.dp + j, w.n_pad * w.dp);
+        }
         before += total;
     }
-    if (blockIdx.x == gridDim.x - 1) {
+    if (blockIdx.x == q.first - 1) {
         if (threadIdx.x == 0) { w.ctrl->count = before; w.ctrl->status = DQ_OK; }
         const int end = (before + kTileK - 1) / kTileK * kTileK;
         for (int i = before + warp; i < end; i += 8)
@@ -283,16 +306,6 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
                 for (int j = lane * 8; j < w.dp; j += 256)
                     *reinterpret_cast<uint4*>(w.hp + (int64_t)t * w.n_pad * w.dp + (int64_t)i * w.dp + j) = make_uint4(0, 0, 0, 0);
     }
-}
-
-// w where tensor maps cannot read it in place (fp32, or rows that do not start on 16 bytes): its bf16 terms, rows padded.
-template <bool F32>
-__global__ void __launch_bounds__(256) vocab_weights_kernel(const void* __restrict__ src, int64_t ld, int d, int64_t V, bool vec, Work w)
-{
-    pdl_prologue();
-    const int lane = threadIdx.x & 31;
-    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < V; r += (int64_t)gridDim.x * 8)
-        copy_row<F32>(src, r * ld, d, vec, w.wp + r * w.dp, V * w.dp, (int)w.dp, lane);
 }
 
 // Joins the (max, sum) pairs of a row's tiles to lse, forms the loss and the two factors of the gradient; a warp per row.
@@ -482,19 +495,19 @@ __global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int d, float 
 // ---- the products ---------------------------------------------------------------------------------------------------
 
 struct MmaArgs {
-    int cols;                // extent of the tile's N axis: classes of the piece (kLse, kProb) or d
-    int kdim;                // extent of the summed axis (kGradW: the number of rows with a target, read on the device)
-    int mdim;                // kGradW: classes of the piece; else the number of rows with a target, read on the device
+    int cols;                // extent of the tile's N axis: classes of the piece, or d (kGrads)
+    int kdim;                // extent of the summed axis: d, or classes of the piece (grad_h; grad_w sums over the rows with a target)
     int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
-    int splits, kps;         // kGradH: pieces of the summed axis, and their length in tiles of K
     int v0;                  // first class of the piece
     int k;                   // targets per row (0: one label)
     float c2;                // log2(e) / T
-    float scale;             // gradients: not 0: the result times scale / (rows with a target)
-    int first, last;         // kGradH: first piece of the vocabulary; the sum is complete and goes to the output
-    int align;               // gradients: rows of the output start on 16 bytes (1), 32 (2) or neither (0)
     const int32_t* eidx;     // targets' classes [n][max(k, 1)], ascending
-    void* out; int64_t ld;   // gradients
+    // kGrads
+    int splits, kps;         // grad_h: pieces of the summed axis in this launch, and their length in tiles of K
+    int first, last;         // grad_h: first, last piece of the vocabulary
+    float scale;             // not 0: the results times scale / (rows with a target)
+    void *gh, *gw; int64_t ld_gh, ld_gw;
+    int align_h, align_w;    // rows of the output start on 16 bytes (1), 32 (2) or neither (0)
 };
 
 // Products of bf16 terms for fp32 operands, smallest first so that the leading one is rounded least: (2,0) (0,2) (1,1) (1,0)
@@ -551,21 +564,52 @@ __device__ __forceinline__ void store_terms(__nv_bfloat16* dst, int64_t plane, c
     for (int p = 0; p < TERMS; ++p) store32(dst + p * plane, e[p], wide);
 }
 
-// One persistent kernel per product.  Warp 0 loads tiles (TMA, 128-byte swizzle), warp 1 issues the matrix instructions, warps
-// 4-11 turn finished accumulators into results while the next products run: tensor memory holds two accumulators of 128 rows by
-// 256 columns.  The tensor cores cut their fp32 sums off toward zero at every step, which over a long K drifts by about
-// K / 16 * 2^-25 of the sum (measured: 1.0e-5 at K = 4096, 6e-5 at 16384); so a sum stays in tensor memory for 512 of K and
-// the epilogue adds these segments in registers, rounded to nearest, while the next one runs (7e-7 at any K, for free).
-// An epilogue thread owns a row's half tile: its maximum and sum need no exchange between threads.
+// Row `at` of a gradient, 128 columns of which `have` exist.
+template <bool F32>
+__device__ __forceinline__ void store_row(void* out, int64_t at, const float (&f)[kHalf], int have, int align)
+{
+#pragma unroll
+    for (int c = 0; c < kHalf; c += 16) {
+        if (align && c + 16 <= have) {
+            if (F32) {
+                uint32_t x[8], y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { x[j] = __float_as_uint(f[c + j]); y[j] = __float_as_uint(f[c + 8 + j]); }
+                store32(static_cast<float*>(out) + at + c, x, align == 2);
+                store32(static_cast<float*>(out) + at + c + 8, y, align == 2);
+            } else {
+                store_terms<1>(static_cast<__nv_bfloat16*>(out) + at + c, 0, f + c, align == 2);
+            }
+        } else if (c < have) {
+#pragma unroll
+            for (int j = c; j < c + 16; ++j) {
+                if (j < have) {
+                    if (F32) static_cast<float*>(out)[at + j] = f[j];
+                    else static_cast<__nv_bfloat16*>(out)[at + j] = __float2bfloat16_rn(f[j]);
+                }
+            }
+        }
+    }
+}
+
+// One persistent kernel per product (kGrads: for the two products that read g).  Warp 0 loads tiles (TMA, 128-byte swizzle), warp 1
+// issues the matrix instructions, warps 4-11 turn finished accumulators into results while the next products run: tensor memory
+// holds two accumulators of 128 rows by 256 columns.  The tensor cores cut their fp32 sums off toward zero at every step, which
+// over a long K drifts by about K / 16 * 2^-25 of the sum (measured: 1.0e-5 at K = 4096, 6e-5 at 16384); so a sum stays in tensor
+// memory for 512 of K and the epilogue adds these segments in registers, rounded to nearest, while the next one runs (7e-7 at any
+// K, for free).  An epilogue thread owns a row's half tile: its maximum and sum need no exchange between threads.
 // CG = 2: two CTAs on neighbouring SMs share a tile of 256 rows.  Each loads its 128 rows and half of the columns' operand; the
 // even one issues for both.
+// Operands: logits h (A) and w (B), both along d.  grad_h: g along the classes, w across.  grad_w: g and h, both across; its K axis
+// are the rows.  ma, mb: operands of the logits or of grad_h; mc, md: those of grad_w.
 template <int CG, int KIND, bool F32>
 __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+                                                           const __grid_constant__ CUtensorMap mc, const __grid_constant__ CUtensorMap md,
                                                            const MmaArgs a, const Work w)
 {
     extern __shared__ char smem_raw[];
     constexpr int NS = stages<CG>(), SB = stage_bytes<CG>(), BN = kTileN / CG;
-    constexpr bool A_MN = KIND == kGradW, B_MN = KIND == kGradH || KIND == kGradW;
+    constexpr bool GRADS = KIND == kGrads;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
     float* const staging = reinterpret_cast<float*>(tail);
@@ -588,6 +632,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         *gave_up = 0;
         mbar_init_fence();
         tma_prefetch_map(&ma); tma_prefetch_map(&mb);
+        if (GRADS) { tma_prefetch_map(&mc); tma_prefetch_map(&md); }
     }
     if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_slot), 512);
     fence_before_sync();
@@ -596,19 +641,23 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
     const uint32_t tmem = *tmem_slot;
     pdl_prologue();
 
+    // Tiles: those whose rows are the rows with a target (kGrads: grad_h, times splits), then grad_w's, shorter ones last.
     const int count = w.ctrl->count;
-    const int mdim = KIND == kGradW ? a.mdim : count;
-    const int kit = ((KIND == kGradW ? count : a.kdim) + kTileK - 1) / kTileK;
-    const int mt = (mdim + 128 * CG - 1) / (128 * CG), nt = (a.cols + kTileN - 1) / kTileN;
-    const int tiles = mt * nt * (KIND == kGradH ? a.splits : 1);
+    const int nt = (a.cols + kTileN - 1) / kTileN, mt = (count + 128 * CG - 1) / (128 * CG), kit = (a.kdim + kTileK - 1) / kTileK;
+    const int mt_w = (a.kdim + 128 * CG - 1) / (128 * CG), kit_w = (count + kTileK - 1) / kTileK;
+    const int tiles_h = mt * nt * (GRADS ? a.splits : 1), tiles = tiles_h + (GRADS ? mt_w * nt : 0);
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    auto tile = [&](int t) {
+        return GRADS && t >= tiles_h ? decode(t - tiles_h, mt_w, nt, kit_w, 0, false) : decode(t, mt, nt, kit, a.kps, GRADS);
+    };
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0 && elect_one()) {
             int s = 0; uint32_t ph = 0; bool ok = true; int issued = 0;
             for (int t = first; t < tiles && ok; t += step) {
-                const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+                const Tile q = tile(t);
+                const bool is_w = GRADS && t >= tiles_h;
                 const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * kTileN + (int)rank * BN;
                 for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
                     const int za = term_a(p), zb = term_b(p);
@@ -617,17 +666,17 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                         const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
                         if (rank == 0) mbar_expect_tx(full(s), CG * SB);
                         const int x = kb * kTileK;
-                        if (!A_MN) {
-                            tma_load<CG>(&ma, dst, bar, x, ym, za);
+                        if (is_w) {
+                            tma_load<CG>(&mc, dst, bar, ym, x, za);
+                            tma_load<CG>(&mc, dst + 8192, bar, ym + 64, x, za);
                         } else {
-                            tma_load<CG>(&ma, dst, bar, ym, x, za);
-                            tma_load<CG>(&ma, dst + 8192, bar, ym + 64, x, za);
+                            tma_load<CG>(&ma, dst, bar, x, ym, za);
                         }
-                        if (!B_MN) {
+                        if (!GRADS) {
                             tma_load<CG>(&mb, dst + 16384, bar, x, yn, zb);
                         } else {
 #pragma unroll
-                            for (int j = 0; j < BN / 64; ++j) tma_load<CG>(&mb, dst + 16384 + j * 8192, bar, yn + j * 64, x, zb);
+                            for (int j = 0; j < BN / 64; ++j) tma_load<CG>(is_w ? &md : &mb, dst + 16384 + j * 8192, bar, yn + j * 64, x, zb);
                         }
                         ++issued;
                         if (++s == NS) { s = 0; ph ^= 1u; }
@@ -643,11 +692,13 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 }
             }
         } else if (warp == 1 && rank == 0 && elect_one()) {
-            constexpr uint32_t idesc = instr_desc_bf16(128 * CG, kTileN, A_MN, B_MN);
-            constexpr uint32_t a_step = A_MN ? 16 * 128 : 32, b_step = B_MN ? 16 * 128 : 32;      // bytes from one K of 16 to the next
             int s = 0, acc = 0; uint32_t ph = 0, aph = 0; bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
-                const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+                const Tile q = tile(t);
+                const bool is_w = GRADS && t >= tiles_h;
+                // bytes from one K of 16 to the next, and between blocks of 64 of an operand that lies across (see smem_desc)
+                const uint32_t idesc = instr_desc_bf16(128 * CG, kTileN, is_w, GRADS), a_step = (is_w ? 16 * 128 : 32) >> 4;
+                constexpr uint32_t b_step = (GRADS ? 16 * 128 : 32) >> 4;
                 const int steps = (q.k1 - q.k0) * a.pairs;
                 for (int i0 = 0; i0 < steps && ok; i0 += kSegment) {
                     const int i1 = min(steps, i0 + kSegment);
@@ -658,10 +709,10 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                         if (!mbar_wait(full(s), ph, gave_up)) { ok = false; break; }
                         fence_after_sync();
                         const uint32_t sa = base + s * SB;
-                        const uint64_t da = smem_desc(sa, A_MN ? 8192 : 16, 1024), db = smem_desc(sa + 16384, B_MN ? 8192 : 16, 1024);
+                        const uint64_t da = smem_desc(sa, is_w ? 8192 : 16, 1024), db = smem_desc(sa + 16384, GRADS ? 8192 : 16, 1024);
 #pragma unroll
                         for (int j = 0; j < kTileK / 16; ++j)
-                            mma_bf16<CG>(d, da + j * (a_step >> 4), db + j * (b_step >> 4), idesc, i != i0 || j != 0);
+                            mma_bf16<CG>(d, da + j * a_step, db + j * b_step, idesc, i != i0 || j != 0);
                         mma_commit<CG>(empty(s));
                         if (++s == NS) { s = 0; ph ^= 1u; }
                     }
@@ -682,14 +733,15 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         const float alpha = a.scale != 0.0f ? a.scale / (float)max(count, 1) : 1.0f;
         int acc = 0; uint32_t aph = 0; bool ok = true;
         for (int t = first; t < tiles && ok; t += step) {
-            const Tile q = decode(t, mt, nt, kit, a.kps, KIND == kGradH);
+            const Tile q = tile(t);
+            const bool is_w = GRADS && t >= tiles_h;
             const int r = q.m * 128 * CG + (int)rank * 128 + quarter * 32 + lane;     // the thread's row of the tile's M axis
             const int col = q.n * kTileN + half * kHalf;                              // its first column
             const int have = a.cols - col;                                            // columns that exist
             // targets of the row: the first one not before the half tile
             int64_t e0 = 0; int pos = 0, next = INT32_MAX; const int ke = a.k > 0 ? a.k : 1, v_at = a.v0 + col;
             float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if ((KIND == kLse || KIND == kProb) && r < count) {       // (kept logits: the rows' kernel looks them up itself)
+            if ((KIND == kLse || KIND == kProb) && r < count) {       // (kept logits: vocab_rows_kernel looks them up)
                 e0 = (int64_t)w.map[r] * ke;
                 int lo = 0, hi = ke;
                 while (lo < hi) { const int mid = (lo + hi) >> 1; if (a.eidx[e0 + mid] < v_at) lo = mid + 1; else hi = mid; }
@@ -775,58 +827,39 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                     }
                     store_terms<F32 ? 3 : 1>(o + c, w.n_pad * w.vc, f + c, true);
                 }
-            } else if (r < mdim) {
-                if (KIND == kGradH && !a.first) {
-                    const float* o = w.dh + ((int64_t)q.split * w.n_pad + r) * w.dq + col;
+            } else {
+                bool out = r < (is_w ? a.kdim : count);
+                if (!is_w && !(a.first && a.last && w.splits == 1)) {
+                    // shares of grad_h: earlier pieces of the vocabulary are in dh, one slot for each split
+                    const int64_t slot = w.n_pad * w.dq;
+                    float* const o = w.dh + (int64_t)r * w.dq + col;
+                    if (out) {
 #pragma unroll
-                    for (int c = 0; c < kHalf; c += 8) {
-                        if (col + c < w.dq) {
-                            float y[8];
-                            load8_rw(o + c, y);
+                        for (int c = 0; c < kHalf; c += 8) {
+                            if (col + c < w.dq) {
+                                float x[8], y[8];
+                                if (!a.first) {
+                                    load8_rw(o + q.split * slot + c, y);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) f[c + j] += y[j];
-                        }
-                    }
-                }
-                if (KIND == kGradH && !a.last) {
-                    float* o = w.dh + ((int64_t)q.split * w.n_pad + r) * w.dq + col;
+                                    for (int j = 0; j < 8; ++j) f[c + j] += y[j];
+                                }
+                                if (!a.last || w.splits > 1) {
 #pragma unroll
-                    for (int c = 0; c < kHalf; c += 8) {
-                        if (col + c < w.dq) {
-                            float x[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) x[j] = f[c + j];
-                            store8(o + c, x);
-                        }
-                    }
-                    continue;
-                }
-                const int64_t at = (int64_t)(KIND == kGradH ? w.map[r] : a.v0 + r) * a.ld + col;
-                if (alpha != 1.0f) {
-#pragma unroll
-                    for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
-                }
-#pragma unroll
-                for (int c = 0; c < kHalf; c += 16) {
-                    if (a.align && c + 16 <= have) {
-                        if (F32) {
-                            uint32_t x[8], y[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) { x[j] = __float_as_uint(f[c + j]); y[j] = __float_as_uint(f[c + 8 + j]); }
-                            store32(static_cast<float*>(a.out) + at + c, x, a.align == 2);
-                            store32(static_cast<float*>(a.out) + at + c + 8, y, a.align == 2);
-                        } else {
-                            store_terms<1>(static_cast<__nv_bfloat16*>(a.out) + at + c, 0, f + c, a.align == 2);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = c; j < c + 16; ++j) {
-                            if (j < have) {
-                                if (F32) static_cast<float*>(a.out)[at + j] = f[j];
-                                else static_cast<__nv_bfloat16*>(a.out)[at + j] = __float2bfloat16_rn(f[j]);
+                                    for (int j = 0; j < 8; ++j) x[j] = f[c + j];
+                                    store8(o + q.split * slot + c, x);
+                                }
                             }
                         }
                     }
+                    if (!a.last || w.splits > 1) out = false;              // vocab_grad_h_kernel adds the splits
+                }
+                if (out) {
+                    if (alpha != 1.0f) {
+#pragma unroll
+                        for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
+                    }
+                    const int64_t row = is_w ? a.v0 + r : w.map[r], ld = is_w ? a.ld_gw : a.ld_gh;
+                    store_row<F32>(is_w ? a.gw : a.gh, row * ld + col, f, have, is_w ? a.align_w : a.align_h);
                 }
             }
         }
@@ -882,12 +915,24 @@ bool device(Device* d)
     return true;
 }
 
+// More shared memory than the default has to be asked for once per kernel and device.
+template <class K>
+bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done)
+{
+    const uint64_t bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(bit, std::memory_order_release);
+    return true;
+}
+
 template <int CG, int KIND, bool F32>
-bool launch_mma_cg(const CUtensorMap& ma, const CUtensorMap& mb, const MmaArgs& a, const Work& w, int64_t tiles, int sms, cudaStream_t st)
+bool launch_mma_cg(const CUtensorMap (&m)[4], const MmaArgs& a, const Work& w, int64_t tiles, const Device& dev, cudaStream_t st)
 {
     auto kernel = vocab_mma_kernel<CG, KIND, F32>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<CG>()) != cudaSuccess) return false;
-    const int64_t units = sms / CG;
+    static std::atomic<uint64_t> allowed{0};
+    if (!allow_smem(kernel, smem_bytes<CG>(), dev.id, allowed)) return false;
+    const int64_t units = dev.sms / CG;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -896,17 +941,17 @@ bool launch_mma_cg(const CUtensorMap& ma, const CUtensorMap& mb, const MmaArgs& 
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(CG * (tiles < units ? tiles : units))); cfg.blockDim = dim3(384);
     cfg.dynamicSmemBytes = smem_bytes<CG>(); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, a, w) == cudaSuccess;
+    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], a, w) == cudaSuccess;
 }
 
-// m: extent of the tile's M axis, nt: tiles along N (times splits).  The columns' operand comes in boxes of 256 / CG rows where it is
-// K-major: `mb` for one CTA, `mb2` for a pair.
+// n: rows; a pair of CTAs shares a tile from 129 rows on.
 template <int KIND, bool F32>
-bool launch_mma(int64_t m, int64_t nt, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mb2, const MmaArgs& a, const Work& w, int sms,
-                cudaStream_t st)
+bool launch_mma(int64_t n, const CUtensorMap (&m)[4], const MmaArgs& a, const Work& w, const Device& dev, cudaStream_t st)
 {
-    if (row_pairs(m) == 2) return launch_mma_cg<2, KIND, F32>(ma, mb2, a, w, (m + 255) / 256 * nt, sms, st);
-    return launch_mma_cg<1, KIND, F32>(ma, mb, a, w, nt, sms, st);
+    const int cg = row_pairs(n);
+    const int64_t nt = (a.cols + kTileN - 1) / kTileN, mt = (n + 128 * cg - 1) / (128 * cg), mt_w = (a.kdim + 128 * cg - 1) / (128 * cg);
+    const int64_t tiles = KIND == kGrads ? nt * (mt * a.splits + mt_w) : nt * mt;
+    return cg == 2 ? launch_mma_cg<2, KIND, F32>(m, a, w, tiles, dev, st) : launch_mma_cg<1, KIND, F32>(m, a, w, tiles, dev, st);
 }
 
 struct Targets { const int32_t* labels; const int32_t* top_idx; const float* top_logits; const float* teacher_lse; float temp; };
@@ -921,62 +966,66 @@ int row_alignment(const void* p, int64_t row_bytes)
 template <bool F32>
 int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
 {
-    const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2;
+    const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2, cg = row_pairs(v->n);
     const int64_t n = v->n, V = v->V;
     const int blocks = dev.sms * 8;
-    auto grid8 = [&](int64_t rows) { return dim3((unsigned)min((int64_t)blocks, (rows + 7) / 8)); };
     bool ok = true;
-    if (k > 0)
-        ok = ok && launch_k(vocab_targets_kernel, dim3((unsigned)min((int64_t)blocks, (n + 3) / 4)), dim3(128), 0, st, t.top_idx, t.top_logits, t.teacher_lse,
-                            1.0f / t.temp, n, k, V, w) == cudaSuccess;
-    const int64_t gblocks = min((int64_t)dev.sms * 2, (n + 7) / 8), per = (n + gblocks - 1) / gblocks;
-    ok = ok && launch_k(vocab_gather_kernel<F32>, dim3((unsigned)((n + per - 1) / per)), dim3(256), 0, st, v->h, v->ld_h, d, k > 0 ? w.tgt : t.labels,
-                        V, n, per, ptr_aligned(v->h, 16) && v->ld_h * elem % 16 == 0, loss, lse, g ? g->gh : nullptr, g ? g->ld_h : 0, w) == cudaSuccess;
-    if (!w.direct_w)
-        ok = ok && launch_k(vocab_weights_kernel<F32>, grid8(V), dim3(256), 0, st, v->w, v->ld_w, d, V, ptr_aligned(v->w, 16) && v->ld_w * elem % 16 == 0, w) == cudaSuccess;
+
+    // targets, rows of h, weights: the first launch copies the weights beside its own work
+    Weights q = {v->w, v->ld_w, V, d, ptr_aligned(v->w, 16) && v->ld_w * elem % 16 == 0, 0};
+    int64_t wblocks = w.direct_w ? 0 : min((int64_t)blocks, (V * (w.dp / 8) + 255) / 256);
+    if (k > 0) {
+        q.first = (int)min((int64_t)blocks, (n + 7) / 8);
+        ok = ok && launch_k(vocab_targets_kernel<F32>, dim3((unsigned)(q.first + wblocks)), dim3(256), 0, st, t.top_idx, t.top_logits, t.teacher_lse, 1.0f / t.temp,
+                            n, k, V, q, w) == cudaSuccess;
+        wblocks = 0;
+    }
+    const int64_t gblocks = min((int64_t)dev.sms * 2, n), per = (n + gblocks - 1) / gblocks;
+    q.first = (int)((n + per - 1) / per);
+    ok = ok && launch_k(vocab_gather_kernel<F32>, dim3((unsigned)(q.first + wblocks)), dim3(256), 0, st, v->h, v->ld_h, d, k > 0 ? w.tgt : t.labels, V, n, per,
+                        ptr_aligned(v->h, 16) && v->ld_h * elem % 16 == 0, loss, lse, g ? g->gh : nullptr, g ? g->ld_h : 0, q, w) == cudaSuccess;
     const __nv_bfloat16* wsrc = w.direct_w ? static_cast<const __nv_bfloat16*>(v->w) : w.wp;
     const int64_t wpitch = w.direct_w ? v->ld_w : w.dp;
 
+    // logits.  m: operand maps; those along d come in boxes of 128 rows of h and 256 / cg rows of w
     MmaArgs a = {};
     a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
-    a.splits = 1; a.kps = 0; a.scale = g && !g->weight ? t.temp : 0.0f;
-    CUtensorMap mh, mw, mw2;
-    ok = ok && make_map(&mh, w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128);
-    ok = ok && make_map(&mw, wsrc, d, V, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wsrc, d, V, wpitch, T, V * wpitch, kTileN / 2);
-    if (!ok) return DQ_ERR_CUDA;
+    a.splits = 1; a.scale = g && !g->weight ? t.temp : 0.0f;
+    CUtensorMap m[4] = {};
+    ok = ok && make_map(&m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128) && make_map(&m[1], wsrc, d, V, wpitch, T, V * wpitch, kTileN / cg);
     a.cols = (int)V; a.kdim = d;
     const float* weight = g ? g->weight : nullptr;
     if (w.keep) {
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
         // cheaper than forming them again (2 d flops, six times that for fp32) and merges the join with what follows it.
-        ok = launch_mma<kLogits, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
+        ok = ok && launch_mma<kLogits, F32>(n, m, a, w, dev, st);
         const int per_row = (int)((w.vc + kRowCols - 1) / kRowCols);
         ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(up(n, kTileK) * per_row)), dim3(256), 0, st, w, V, k, per_row, t.labels, weight, t.temp, a.c2,
                             loss, lse) == cudaSuccess;
     } else {
-        ok = launch_mma<kLse, F32>(n, w.vtiles, mh, mw, mw2, a, w, dev.sms, st);
-        ok = ok && launch_k(vocab_join_kernel, grid8(n), dim3(256), 0, st, w, k, t.labels, weight, t.temp, a.c2, loss, lse) == cudaSuccess;
+        ok = ok && launch_mma<kLse, F32>(n, m, a, w, dev, st);
+        ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, t.labels, weight, t.temp, a.c2, loss, lse)
+                       == cudaSuccess;
     }
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
 
-    CUtensorMap mg_k, mg_mn, mw_mn, mh_mn;
-    const int ntd = (d + kTileN - 1) / kTileN;
-    ok = ok && make_map(&mg_k, w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128);
-    ok = ok && make_map(&mg_mn, w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK);
-    ok = ok && make_map(&mh_mn, w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
+    // gradients, a piece of the vocabulary at a time
+    CUtensorMap u[4] = {};
+    ok = ok && make_map(&u[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128) && make_map(&u[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
+         make_map(&u[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
+    a.gh = g->gh; a.gw = g->gw; a.ld_gh = g->ld_h; a.ld_gw = g->ld_w; a.kps = w.kps;
+    a.align_h = row_alignment(g->gh, g->ld_h * elem); a.align_w = row_alignment(g->gw, g->ld_w * elem);
     for (int64_t v0 = 0; v0 < V && ok; v0 += w.vc) {
         const int vn = (int)min(w.vc, V - v0);
         const __nv_bfloat16* wv = wsrc + v0 * wpitch;
-        ok = make_map(&mw, wv, d, vn, wpitch, T, V * wpitch, kTileN) && make_map(&mw2, wv, d, vn, wpitch, T, V * wpitch, kTileN / 2) &&
-             make_map(&mw_mn, wv, d, vn, wpitch, T, V * wpitch, kTileK);
-        a.v0 = (int)v0; a.cols = vn; a.kdim = d; a.splits = 1;
-        if (!w.keep) ok = ok && launch_mma<kProb, F32>(n, (vn + kTileN - 1) / kTileN, mh, mw, mw2, a, w, dev.sms, st);
-        a.cols = d; a.mdim = vn; a.out = g->gw; a.ld = g->ld_w; a.align = row_alignment(g->gw, g->ld_w * elem);
-        ok = ok && launch_mma<kGradW, F32>(vn, ntd, mg_mn, mh_mn, mh_mn, a, w, dev.sms, st);
-        a.kdim = vn; a.kps = w.kps; a.first = v0 == 0; a.last = w.splits == 1 && v0 + w.vc >= V;
-        a.out = g->gh; a.ld = g->ld_h; a.align = row_alignment(g->gh, g->ld_h * elem);
+        a.v0 = (int)v0;
+        if (!w.keep) {
+            a.cols = vn; a.kdim = d; a.splits = 1;
+            ok = make_map(&m[1], wv, d, vn, wpitch, T, V * wpitch, kTileN / cg) && launch_mma<kProb, F32>(n, m, a, w, dev, st);
+        }
+        a.cols = d; a.kdim = vn; a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
-        ok = ok && launch_mma<kGradH, F32>(n, (int64_t)ntd * a.splits, mg_k, mw_mn, mw_mn, a, w, dev.sms, st);
+        ok = ok && make_map(&u[1], wv, d, vn, wpitch, T, V * wpitch, kTileK) && launch_mma<kGrads, F32>(n, u, a, w, dev, st);
     }
     if (w.splits > 1) {
         const int64_t need = (n * ((d + 3) / 4) + 255) / 256;
@@ -1033,7 +1082,18 @@ int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
     Device dev;
     if (check_vocab(v) != DQ_OK) return -1;
     if (!device(&dev)) { cudaGetLastError(); return -1; }
-    return carve(v, grad != 0, dev.sms).bytes;
+    // enough for every number of rows up to n: the parts' sizes do not all grow with it (pieces, splits, the one-launch form)
+    int64_t most = 0;
+    dq_vocab u = *v;
+    auto see = [&](int64_t n) {
+        if (n < 0 || n > v->n) return;
+        u.n = n;
+        const int64_t bytes = carve(&u, grad != 0, dev.sms).bytes;
+        if (bytes > most) most = bytes;
+    };
+    for (int64_t n = 0; n < v->n; n += 256) see(n);
+    see(v->n); see(128);
+    return most;
 }
 
 int dq_xent_loss(const dq_vocab* v, const int32_t* labels, float* loss, float* lse, void* stream)
