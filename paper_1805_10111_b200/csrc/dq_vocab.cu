@@ -24,12 +24,21 @@ using namespace mma;
 
 // What a product's epilogue does: (max, sum) of the logits; the same and the logits; the logits' gradient; both gradients.
 enum { kLse = 0, kLogits = 1, kProb = 2, kGrads = 3 };
-constexpr int kTileN = 256, kTileK = 64;
+constexpr int kTileN = 256, kNarrow = 64, kTileK = 64;    // columns of a tile where there are tiles enough for the SMs, and where not
 constexpr int kMaxTop = DQ_VOCAB_MAX_TOP;
-constexpr int kHalf = kTileN / 2;                         // columns of an epilogue thread
 constexpr int kPiece = 16;                                // columns staged at a time where a row has targets among them
 constexpr int kSegment = 8;                               // tiles of K summed in tensor memory before the sum moves to registers
 constexpr int64_t kGradBytes = 256ll << 20;               // bound on the piece of g kept between products
+
+// Tiles of a product over m rows (of M) and `cols` columns.  128 by 64 where tiles of 256 columns would leave half of the SMs without one:
+// more SMs then share the loads, which is what bounds such products (64 x 512 x 2000: xx us against yy).  Otherwise 256 columns, shared by a
+// pair of CTAs unless one CTA's 128 rows hold them all.
+struct Shape { int tn, cg; };
+Shape tile_shape(int64_t n, int64_t m, int64_t cols, int sms)
+{
+    if ((m + 127) / 128 * ((cols + kTileN - 1) / kTileN) < sms / 2) return {kNarrow, 1};
+    return {kTileN, n > 128 ? 2 : 1};
+}
 
 struct Ctrl { int status; int count; };                   // head of the workspace: sticky status, rows with a target
 
@@ -47,15 +56,13 @@ struct Work {
     __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
     float* dh;                     // [splits][n_pad][dq] sums of grad_h
     // sizes
-    int terms; int64_t n_pad, dp, dq, vc; int vtiles, parts, splits, kps; bool direct_w, keep;
+    int terms; int64_t n_pad, dp, dq, vc; int parts, splits, kps; bool direct_w, keep;
+    Shape logits, grads;           // tiles of the products
     int64_t bytes;
 };
 
 bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
-
-// CTAs that share a tile whose M axis are the rows: a pair, unless one CTA's 128 rows hold them all.
-int row_pairs(int64_t n) { return n > 128 ? 2 : 1; }
 
 Work carve(const dq_vocab* v, bool grad, int sms)
 {
@@ -64,7 +71,8 @@ Work carve(const dq_vocab* v, bool grad, int sms)
     w.terms = f32 ? 3 : 1;
     w.n_pad = up(v->n > 0 ? v->n : 1, 256);
     w.dp = up(v->d, 8); w.dq = up(v->d, 8);
-    w.vtiles = (int)((v->V + kTileN - 1) / kTileN); w.parts = 2 * w.vtiles;
+    w.logits = tile_shape(v->n, v->n, v->V, sms);
+    w.parts = 2 * (int)((v->V + w.logits.tn - 1) / w.logits.tn);
     w.direct_w = !f32 && ptr_aligned(v->w, 16) && v->ld_w % 8 == 0;
     const int k = v->k > 0 ? v->k : 1;
     int64_t at = 0;
@@ -91,8 +99,9 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         w.keep = w.vc >= v->V && 4 * w.n_pad * w.vc <= kGradBytes;
         if (w.keep) w.z = (float*)take(4 * w.n_pad * w.vc);
         // few rows: grad_h has fewer tiles than the GPU has SMs, so its sum over the vocabulary is split and joined
-        const int cg = row_pairs(v->n), units = sms / cg;
-        const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + kTileN - 1) / kTileN));
+        w.grads = tile_shape(v->n, w.vc > v->n ? w.vc : v->n, v->d, sms);
+        const int cg = w.grads.cg, tn = w.grads.tn, units = sms / cg;
+        const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + tn - 1) / tn));
         const int kit = (int)(w.vc / kTileK);
         int splits = tiles < 1 || tiles >= units ? 1 : units / tiles;
         // at least 512 classes to a split (256 for fp32, which takes six products of each): below that the shares' traffic outweighs
@@ -515,10 +524,15 @@ struct MmaArgs {
 __device__ __forceinline__ int term_a(int p) { return (0x001102 >> (4 * p)) & 15; }
 __device__ __forceinline__ int term_b(int p) { return (0x010120 >> (4 * p)) & 15; }
 
-template <int CG> __host__ __device__ constexpr int stage_bytes() { return 128 * 128 + (kTileN / CG) * 128; }
-template <int CG> __host__ __device__ constexpr int stages() { return CG == 1 ? 4 : 6; }
-constexpr int kStagingBytes = 8 * kPiece * 32 * 4;
-template <int CG> __host__ __device__ constexpr int smem_bytes() { return 1024 + stages<CG>() * stage_bytes<CG>() + kStagingBytes + 256; }
+// Shared memory of a product: NS stages of both operands' tiles, and for each epilogue warp either one piece of columns (targets
+// are looked up in it) or two buffers of 32 rows by 128 bytes on their way out by TMA.
+template <int CG, int KIND, int TN> struct Smem {
+    static constexpr bool kTmaOut = TN == kTileN && (KIND == kLogits || KIND == kGrads);
+    static constexpr int kStage = 128 * 128 + TN / CG * 128;
+    static constexpr int kStages = TN == kNarrow ? 8 : CG == 1 ? (kTmaOut ? 3 : 4) : (kTmaOut ? 5 : 6);
+    static constexpr int kStaging = 8 * (kTmaOut ? 2 * 4096 : kPiece * 32 * 4);
+    static constexpr int kBytes = 1024 + kStages * kStage + kStaging + 256;
+};
 
 struct Tile { int m, n, split, k0, k1; };
 
@@ -564,8 +578,8 @@ __device__ __forceinline__ void store_terms(__nv_bfloat16* dst, int64_t plane, c
     for (int p = 0; p < TERMS; ++p) store32(dst + p * plane, e[p], wide);
 }
 
-// Row `at` of a gradient, 128 columns of which `have` exist.
-template <bool F32>
+// A thread's columns of a row of a gradient, from position `at`; `have` of them exist.
+template <bool F32, int kHalf>
 __device__ __forceinline__ void store_row(void* out, int64_t at, const float (&f)[kHalf], int have, int align)
 {
 #pragma unroll
@@ -602,18 +616,19 @@ __device__ __forceinline__ void store_row(void* out, int64_t at, const float (&f
 // even one issues for both.
 // Operands: logits h (A) and w (B), both along d.  grad_h: g along the classes, w across.  grad_w: g and h, both across; its K axis
 // are the rows.  ma, mb: operands of the logits or of grad_h; mc, md: those of grad_w.
-template <int CG, int KIND, bool F32>
+template <int CG, int KIND, bool F32, int TN>
 __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
                                                            const __grid_constant__ CUtensorMap mc, const __grid_constant__ CUtensorMap md,
-                                                           const MmaArgs a, const Work w)
+                                                           const __grid_constant__ CUtensorMap mo, const MmaArgs a, const Work w)
 {
     extern __shared__ char smem_raw[];
-    constexpr int NS = stages<CG>(), SB = stage_bytes<CG>(), BN = kTileN / CG;
+    using S = Smem<CG, KIND, TN>;
+    constexpr int NS = S::kStages, SB = S::kStage, BN = TN / CG, kHalf = TN / 2;
     constexpr bool GRADS = KIND == kGrads;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
     float* const staging = reinterpret_cast<float*>(tail);
-    uint64_t* const bars = reinterpret_cast<uint64_t*>(tail + kStagingBytes);     // full[NS], empty[NS], tfull[2], tempty[2], drain
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(tail + S::kStaging);       // full[NS], empty[NS], tfull[2], tempty[2], drain
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8 * s; };
     auto empty = [&](int s) { return bar0 + 8 * (NS + s); };
@@ -633,8 +648,9 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         mbar_init_fence();
         tma_prefetch_map(&ma); tma_prefetch_map(&mb);
         if (GRADS) { tma_prefetch_map(&mc); tma_prefetch_map(&md); }
+        if (S::kTmaOut) tma_prefetch_map(&mo);
     }
-    if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_slot), 512);
+    if (warp == 2) tmem_alloc<CG>(smem_u32(tmem_slot), 2 * TN);
     fence_before_sync();
     if (CG == 2) cluster_sync(); else __syncthreads();
     fence_after_sync();
@@ -643,7 +659,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
 
     // Tiles: those whose rows are the rows with a target (kGrads: grad_h, times splits), then grad_w's, shorter ones last.
     const int count = w.ctrl->count;
-    const int nt = (a.cols + kTileN - 1) / kTileN, mt = (count + 128 * CG - 1) / (128 * CG), kit = (a.kdim + kTileK - 1) / kTileK;
+    const int nt = (a.cols + TN - 1) / TN, mt = (count + 128 * CG - 1) / (128 * CG), kit = (a.kdim + kTileK - 1) / kTileK;
     const int mt_w = (a.kdim + 128 * CG - 1) / (128 * CG), kit_w = (count + kTileK - 1) / kTileK;
     const int tiles_h = mt * nt * (GRADS ? a.splits : 1), tiles = tiles_h + (GRADS ? mt_w * nt : 0);
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -658,7 +674,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
-                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * kTileN + (int)rank * BN;
+                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * TN + (int)rank * BN;
                 for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
                     const int za = term_a(p), zb = term_b(p);
                     for (int kb = q.k0; kb < q.k1; ++kb) {
@@ -697,14 +713,14 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
                 // bytes from one K of 16 to the next, and between blocks of 64 of an operand that lies across (see smem_desc)
-                const uint32_t idesc = instr_desc_bf16(128 * CG, kTileN, is_w, GRADS), a_step = (is_w ? 16 * 128 : 32) >> 4;
+                const uint32_t idesc = instr_desc_bf16(128 * CG, TN, is_w, GRADS), a_step = (is_w ? 16 * 128 : 32) >> 4;
                 constexpr uint32_t b_step = (GRADS ? 16 * 128 : 32) >> 4;
                 const int steps = (q.k1 - q.k0) * a.pairs;
                 for (int i0 = 0; i0 < steps && ok; i0 += kSegment) {
                     const int i1 = min(steps, i0 + kSegment);
                     if (!mbar_wait(tempty(acc), aph ^ 1u, gave_up)) { ok = false; break; }
                     fence_after_sync();
-                    const uint32_t d = tmem + acc * kTileN;
+                    const uint32_t d = tmem + acc * TN;
                     for (int i = i0; i < i1; ++i) {
                         if (!mbar_wait(full(s), ph, gave_up)) { ok = false; break; }
                         fence_after_sync();
@@ -730,13 +746,34 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         float* const stage = staging + (warp - 4) * kPiece * 32 + lane;       // [column][lane]
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        // out by TMA: the row goes to shared memory in pieces of 128 bytes (128-byte swizzle, two buffers in turn), one lane sends 32
+        // rows of it.  Stores straight from registers cost the L1 a pass for each row (64 x 2048 x 65536: 155 us against 1xx)
+        char* const obuf = tail + (warp - 4) * 8192;
+        int turn = 0;
+        auto send = [&](const float* f, bool f32, int x, int y) {
+            if (lane == 0) tma_store_wait_read<1>();
+            __syncwarp();
+            char* const row = obuf + turn * 4096 + lane * 128;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                uint4 v;
+                if (f32) v = make_uint4(__float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]), __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
+                else v = make_uint4(pack2(__float2bfloat16_rn(f[8 * c]), __float2bfloat16_rn(f[8 * c + 1])), pack2(__float2bfloat16_rn(f[8 * c + 2]), __float2bfloat16_rn(f[8 * c + 3])),
+                                    pack2(__float2bfloat16_rn(f[8 * c + 4]), __float2bfloat16_rn(f[8 * c + 5])), pack2(__float2bfloat16_rn(f[8 * c + 6]), __float2bfloat16_rn(f[8 * c + 7])));
+                *reinterpret_cast<uint4*>(row + ((c ^ (lane & 7)) << 4)) = v;
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) tma_store(&mo, smem_u32(obuf + turn * 4096), x, y);
+            turn ^= 1;
+        };
         const float alpha = a.scale != 0.0f ? a.scale / (float)max(count, 1) : 1.0f;
         int acc = 0; uint32_t aph = 0; bool ok = true;
         for (int t = first; t < tiles && ok; t += step) {
             const Tile q = tile(t);
             const bool is_w = GRADS && t >= tiles_h;
             const int r = q.m * 128 * CG + (int)rank * 128 + quarter * 32 + lane;     // the thread's row of the tile's M axis
-            const int col = q.n * kTileN + half * kHalf;                              // its first column
+            const int col = q.n * TN + half * kHalf;                                  // its first column
             const int have = a.cols - col;                                            // columns that exist
             // targets of the row: the first one not before the half tile
             int64_t e0 = 0; int pos = 0, next = INT32_MAX; const int ke = a.k > 0 ? a.k : 1, v_at = a.v0 + col;
@@ -757,7 +794,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 __syncwarp();
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(tfull(acc), aph, gave_up))) { ok = false; break; }    // the warp leaves as one
                 fence_after_sync();
-                const uint32_t d = tmem + lanes + acc * kTileN + half * kHalf;
+                const uint32_t d = tmem + lanes + acc * TN + half * kHalf;
 #pragma unroll
                 for (int c = 0; c < kHalf; c += 32) {
                     uint32_t v[32];
@@ -776,7 +813,10 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             if (KIND == kLse || KIND == kLogits) {
 #pragma unroll
                 for (int c = 0; c < kHalf; c += kPiece) {
-                    if (KIND == kLogits) {
+                    if (S::kTmaOut) {
+                        // (rows behind the last one hold nothing that is read; they stay inside n_pad)
+                        if (c % 32 == 0 && c < have) send(f + c, true, col + c, r - lane);
+                    } else if (KIND == kLogits) {
                         if (r < count && c < have) {
                             float* o = w.z + (int64_t)r * w.vc + col + c;
                             float x[8], y[8];
@@ -853,24 +893,29 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                     }
                     if (!a.last || w.splits > 1) out = false;              // vocab_grad_h_kernel adds the splits
                 }
-                if (out) {
-                    if (alpha != 1.0f) {
+                if (alpha != 1.0f) {
 #pragma unroll
-                        for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
-                    }
+                    for (int j = 0; j < kHalf; ++j) f[j] *= alpha;
+                }
+                if (S::kTmaOut && is_w && a.align_w) {
+#pragma unroll
+                    for (int c = 0; c < kHalf; c += F32 ? 32 : 64)
+                        if (c < have && r - lane < a.kdim) send(f + c, F32, col + c, r - lane);
+                } else if (out) {
                     const int64_t row = is_w ? a.v0 + r : w.map[r], ld = is_w ? a.ld_gw : a.ld_gh;
                     store_row<F32>(is_w ? a.gw : a.gh, row * ld + col, f, have, is_w ? a.align_w : a.align_h);
                 }
             }
         }
     }
+    if (S::kTmaOut && warp >= 4 && lane == 0) tma_store_wait_all();
     __syncwarp();
     __syncthreads();
     if (threadIdx.x == 0 && *gave_up) set_status(&w.ctrl->status, DQ_ERR_TIMEOUT);
     fence_before_sync();
     if (CG == 2) cluster_sync();
     fence_after_sync();
-    if (warp == 2) tmem_free<CG>(tmem, 512);
+    if (warp == 2) tmem_free<CG>(tmem, 2 * TN);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -900,6 +945,17 @@ bool make_map(CUtensorMap* map, const void* p, int64_t inner, int64_t rows, int6
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The output's map: boxes of 32 rows by 128 bytes.
+bool make_out_map(CUtensorMap* map, bool f32, void* p, int64_t inner, int64_t rows, int64_t pitch)
+{
+    const int elem = f32 ? 4 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch * elem};
+    const cuuint32_t boxes[2] = {(cuuint32_t)(128 / elem), 32}, ones[2] = {1, 1};
+    EncodeTiled f = encode_tiled();
+    return f && f(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Device { int id = -1, sms = 0; };
 bool device(Device* d)
 {
@@ -926,12 +982,16 @@ bool allow_smem(K kernel, int bytes, int dev, std::atomic<uint64_t>& done)
     return true;
 }
 
-template <int CG, int KIND, bool F32>
-bool launch_mma_cg(const CUtensorMap (&m)[4], const MmaArgs& a, const Work& w, int64_t tiles, const Device& dev, cudaStream_t st)
+// m: operands of the logits or of grad_h, operands of grad_w, output (see the kernel).
+struct Maps { CUtensorMap m[5]; };
+
+template <int CG, int KIND, bool F32, int TN>
+bool launch_mma_cg(const Maps& m, const MmaArgs& a, const Work& w, int64_t tiles, const Device& dev, cudaStream_t st)
 {
-    auto kernel = vocab_mma_kernel<CG, KIND, F32>;
+    auto kernel = vocab_mma_kernel<CG, KIND, F32, TN>;
+    constexpr int smem = Smem<CG, KIND, TN>::kBytes;
     static std::atomic<uint64_t> allowed{0};
-    if (!allow_smem(kernel, smem_bytes<CG>(), dev.id, allowed)) return false;
+    if (!allow_smem(kernel, smem, dev.id, allowed)) return false;
     const int64_t units = dev.sms / CG;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -940,18 +1000,19 @@ bool launch_mma_cg(const CUtensorMap (&m)[4], const MmaArgs& a, const Work& w, i
     attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(CG * (tiles < units ? tiles : units))); cfg.blockDim = dim3(384);
-    cfg.dynamicSmemBytes = smem_bytes<CG>(); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], a, w) == cudaSuccess;
+    cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, m.m[0], m.m[1], m.m[2], m.m[3], m.m[4], a, w) == cudaSuccess;
 }
 
-// n: rows; a pair of CTAs shares a tile from 129 rows on.
+// n: rows.
 template <int KIND, bool F32>
-bool launch_mma(int64_t n, const CUtensorMap (&m)[4], const MmaArgs& a, const Work& w, const Device& dev, cudaStream_t st)
+bool launch_mma(int64_t n, const Shape& s, const Maps& m, const MmaArgs& a, const Work& w, const Device& dev, cudaStream_t st)
 {
-    const int cg = row_pairs(n);
-    const int64_t nt = (a.cols + kTileN - 1) / kTileN, mt = (n + 128 * cg - 1) / (128 * cg), mt_w = (a.kdim + 128 * cg - 1) / (128 * cg);
+    const int64_t nt = (a.cols + s.tn - 1) / s.tn, mt = (n + 128 * s.cg - 1) / (128 * s.cg), mt_w = (a.kdim + 128 * s.cg - 1) / (128 * s.cg);
     const int64_t tiles = KIND == kGrads ? nt * (mt * a.splits + mt_w) : nt * mt;
-    return cg == 2 ? launch_mma_cg<2, KIND, F32>(m, a, w, tiles, dev, st) : launch_mma_cg<1, KIND, F32>(m, a, w, tiles, dev, st);
+    // (narrow logits are fewer than 74 x 128 x 256: always kept, so that kProb has none of them)
+    if (KIND != kProb && s.tn == kNarrow) return launch_mma_cg<1, KIND, F32, KIND == kProb ? kTileN : kNarrow>(m, a, w, tiles, dev, st);
+    return s.cg == 2 ? launch_mma_cg<2, KIND, F32, kTileN>(m, a, w, tiles, dev, st) : launch_mma_cg<1, KIND, F32, kTileN>(m, a, w, tiles, dev, st);
 }
 
 struct Targets { const int32_t* labels; const int32_t* top_idx; const float* top_logits; const float* teacher_lse; float temp; };
@@ -966,7 +1027,7 @@ int row_alignment(const void* p, int64_t row_bytes)
 template <bool F32>
 int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
 {
-    const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2, cg = row_pairs(v->n);
+    const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2;
     const int64_t n = v->n, V = v->V;
     const int blocks = dev.sms * 8;
     bool ok = true;
@@ -987,32 +1048,34 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     const __nv_bfloat16* wsrc = w.direct_w ? static_cast<const __nv_bfloat16*>(v->w) : w.wp;
     const int64_t wpitch = w.direct_w ? v->ld_w : w.dp;
 
-    // logits.  m: operand maps; those along d come in boxes of 128 rows of h and 256 / cg rows of w
+    // logits: boxes along d, of 128 rows of h and a CTA's share of a tile's rows of w
     MmaArgs a = {};
     a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
     a.splits = 1; a.scale = g && !g->weight ? t.temp : 0.0f;
-    CUtensorMap m[4] = {};
-    ok = ok && make_map(&m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128) && make_map(&m[1], wsrc, d, V, wpitch, T, V * wpitch, kTileN / cg);
+    Maps m = {};
+    ok = ok && make_map(&m.m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128) &&
+         make_map(&m.m[1], wsrc, d, V, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg);
+    if (w.keep) ok = ok && make_out_map(&m.m[4], true, w.z, w.vc, w.n_pad, w.vc);
     a.cols = (int)V; a.kdim = d;
     const float* weight = g ? g->weight : nullptr;
     if (w.keep) {
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
         // cheaper than forming them again (2 d flops, six times that for fp32) and merges the join with what follows it.
-        ok = ok && launch_mma<kLogits, F32>(n, m, a, w, dev, st);
+        ok = ok && launch_mma<kLogits, F32>(n, w.logits, m, a, w, dev, st);
         const int per_row = (int)((w.vc + kRowCols - 1) / kRowCols);
         ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(up(n, kTileK) * per_row)), dim3(256), 0, st, w, V, k, per_row, t.labels, weight, t.temp, a.c2,
                             loss, lse) == cudaSuccess;
     } else {
-        ok = ok && launch_mma<kLse, F32>(n, m, a, w, dev, st);
+        ok = ok && launch_mma<kLse, F32>(n, w.logits, m, a, w, dev, st);
         ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, t.labels, weight, t.temp, a.c2, loss, lse)
                        == cudaSuccess;
     }
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
 
     // gradients, a piece of the vocabulary at a time
-    CUtensorMap u[4] = {};
-    ok = ok && make_map(&u[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128) && make_map(&u[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
-         make_map(&u[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
+    Maps u = {};
+    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
+         make_map(&u.m[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
     a.gh = g->gh; a.gw = g->gw; a.ld_gh = g->ld_h; a.ld_gw = g->ld_w; a.kps = w.kps;
     a.align_h = row_alignment(g->gh, g->ld_h * elem); a.align_w = row_alignment(g->gw, g->ld_w * elem);
     for (int64_t v0 = 0; v0 < V && ok; v0 += w.vc) {
@@ -1021,11 +1084,13 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         a.v0 = (int)v0;
         if (!w.keep) {
             a.cols = vn; a.kdim = d; a.splits = 1;
-            ok = make_map(&m[1], wv, d, vn, wpitch, T, V * wpitch, kTileN / cg) && launch_mma<kProb, F32>(n, m, a, w, dev, st);
+            ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg) && launch_mma<kProb, F32>(n, w.logits, m, a, w, dev, st);
         }
         a.cols = d; a.kdim = vn; a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
-        ok = ok && make_map(&u[1], wv, d, vn, wpitch, T, V * wpitch, kTileK) && launch_mma<kGrads, F32>(n, u, a, w, dev, st);
+        u.m[4] = u.m[3];                                   // (a valid map, though one for grad_w is not used without alignment)
+        if (a.align_w) ok = ok && make_out_map(&u.m[4], F32, static_cast<char*>(g->gw) + v0 * g->ld_w * elem, d, vn, g->ld_w);
+        ok = ok && make_map(&u.m[1], wv, d, vn, wpitch, T, V * wpitch, kTileK) && launch_mma<kGrads, F32>(n, w.grads, u, a, w, dev, st);
     }
     if (w.splits > 1) {
         const int64_t need = (n * ((d + 3) / 4) + 255) / 256;
@@ -1091,8 +1156,8 @@ int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
         const int64_t bytes = carve(&u, grad != 0, dev.sms).bytes;
         if (bytes > most) most = bytes;
     };
-    for (int64_t n = 0; n < v->n; n += 256) see(n);
-    see(v->n); see(128);
+    for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128
+    see(v->n);
     return most;
 }
 
