@@ -40,7 +40,7 @@ Shape tile_shape(int64_t n, int64_t m, int64_t cols, int sms)
     return {kTileN, n > 128 ? 2 : 1};
 }
 
-struct Ctrl { int status; int count; };                   // head of the workspace: sticky status, rows with a target
+struct Ctrl { int status; int count; uint32_t mask; };    // head of the workspace: status, rows with a target, which (few rows)
 
 // The workspace, carved from the caller's buffer (all parts 256-byte aligned).
 struct Work {
@@ -54,9 +54,12 @@ struct Work {
     float* z;                      // [n_pad][vc] the logits, where they are few enough to be kept (see run_loss)
     float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, log2 units
     __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
+    float* gf;                     // few rows: the logits' gradient [V][few]
     float* dh;                     // [splits][n_pad][dq] sums of grad_h
     // sizes
     int terms; int64_t n_pad, dp, dq, vc; int parts, splits, kps; bool direct_w, keep;
+    int few;                       // rows that the products of few rows work on, 2 or 8; 0: tensor cores
+    int chunks; int64_t span;      // their gradients' blocks: pieces of 128 columns, classes of a block
     Shape logits, grads;           // tiles of the products
     int64_t bytes;
 };
@@ -64,12 +67,16 @@ struct Work {
 bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
+constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
+__host__ __device__ constexpr int few_blocks(int rows) { return rows == 2 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
+
 Work carve(const dq_vocab* v, bool grad, int sms)
 {
     Work w = {};
     const bool f32 = v->format == DQ_DENSE_F32;
     w.terms = f32 ? 3 : 1;
-    w.n_pad = up(v->n > 0 ? v->n : 1, 256);
+    const bool few = f32 && v->n >= 1 && v->n <= kFewRows;
+    w.n_pad = few ? kFewRows : up(v->n > 0 ? v->n : 1, 256);
     w.dp = up(v->d, 8); w.dq = up(v->d, 8);
     w.logits = tile_shape(v->n, v->n, v->V, sms);
     w.parts = 2 * (int)((v->V + w.logits.tn - 1) / w.logits.tn);
@@ -85,6 +92,26 @@ Work carve(const dq_vocab* v, bool grad, int sms)
     if (v->k > 0) {
         w.tgt = (int32_t*)take(4 * w.n_pad); w.emass = (float*)take(4 * w.n_pad);
         w.eidx = (int32_t*)take(4 * w.n_pad * k); w.eq = (float*)take(4 * w.n_pad * k); w.elq = (float*)take(4 * w.n_pad * k);
+    }
+    if (few) {
+        w.few = v->n <= 2 ? 2 : 8;
+        const int64_t groups = (v->V + (w.few == 8 ? 31 : 63)) / (w.few == 8 ? 32 : 64);       // classes that a block takes at a time
+        w.parts = (int)(groups < 2 * sms ? groups : 2 * sms);
+        w.vc = up(v->V, 8);
+        w.z = (float*)take(4 * w.few * w.vc);
+        w.part = (float2*)take(8 * (int64_t)w.few * w.parts);
+        if (grad) {
+            w.gf = (float*)take(4 * w.few * v->V);
+            w.chunks = (int)((v->d + 127) / 128);
+            w.splits = few_blocks(w.few) * sms / w.chunks;                 // one wave of blocks
+            if (w.splits < 1) w.splits = 1;
+            if (w.splits > (v->V + 63) / 64) w.splits = (int)((v->V + 63) / 64);
+            w.span = (v->V + w.splits - 1) / w.splits;
+            w.splits = (int)((v->V + w.span - 1) / w.span);
+            w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
+        }
+        w.bytes = at;
+        return w;
     }
     w.hp = (__nv_bfloat16*)take(2 * w.terms * w.n_pad * w.dp);
     if (!w.direct_w) w.wp = (__nv_bfloat16*)take(2 * w.terms * v->V * w.dp);
@@ -399,72 +426,77 @@ __device__ __forceinline__ float2 block_join(const float2* p, int parts)
     return make_float2(m, s);
 }
 
-// Kept logits to their gradient: a block takes 2048 columns of a row (and joins the row's pairs itself: a few KB from L2 against
-// a launch).  Column block 0 also writes the loss.  Rows behind the last one, up to a whole tile of K, and columns behind the
+// Kept logits to their gradient: a block takes part of a row's columns, 2048 at a time, and joins the row's pairs itself (a few KB
+// from L2 against a launch).  Part 0 also writes the loss.  Rows behind the last one, up to a whole tile of K, and columns behind the
 // vocabulary are zeros: the gradients' products read them.
 constexpr int kRowCols = 2048;
 template <bool F32>
-__global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int64_t V, int k, int blocks_per_row, const int32_t* __restrict__ labels,
+__global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, int parts_per_row, const int32_t* __restrict__ labels,
                                                          const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
                                                          float* __restrict__ lse)
 {
     pdl_prologue();
     constexpr int TERMS = F32 ? 3 : 1;
-    const int count = w.ctrl->count, i = blockIdx.x / blocks_per_row, cb = blockIdx.x % blocks_per_row;
+    const int count = w.ctrl->count, i = blockIdx.x / parts_per_row, part = blockIdx.x % parts_per_row;
     if (i >= (count + kTileK - 1) / kTileK * kTileK) return;
     const int64_t plane = w.n_pad * w.vc;
-    __nv_bfloat16* g = w.g + (int64_t)i * w.vc;
-    const int64_t col = (int64_t)cb * kRowCols + threadIdx.x * 8;
-    float f[8];
-    float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    int64_t row = 0;
-    const float* z = w.z + (int64_t)i * w.vc;
-    if (i < count) {
-        if (col < w.vc) load8_rw(z + col, f);
-        row = w.map[i];
-        const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts);
-        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
-        const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f;
-        rc = make_float4(ms.x, wt * mass / ms.y, wt, 0.0f);
-        if (cb == 0 && threadIdx.x < 32) {
-            double sum = 0.0;
-            if (k == 0) {
-                sum = l - (double)z[labels[row]];
-            } else {
-                for (int j = threadIdx.x; j < k; j += 32) {
-                    const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
-                    if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
-                }
+    const int vc = (int)w.vc, span = (vc / parts_per_row + kRowCols) / kRowCols * kRowCols, lo = part * span, hi = min(vc, lo + span);
+    if (lo >= hi) return;
+    __nv_bfloat16* const g = w.g + (int64_t)i * vc;
+    if (i >= count) {
+        for (int col = lo + threadIdx.x * 8; col < hi; col += kRowCols)
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                sum *= (double)temp * (double)temp;
-            }
-            if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
-        }
+            for (int p = 0; p < TERMS; ++p) *reinterpret_cast<uint4*>(g + p * plane + col) = make_uint4(0, 0, 0, 0);
+        return;
     }
-    if (col < w.vc) {
-        uint32_t e[TERMS][4];
+    const float* const z = w.z + (int64_t)i * vc;
+    float f[8];
+    int col = lo + threadIdx.x * 8;
+    if (col < hi) load8_rw(z + col, f);                            // on its way while the pairs are joined
+    const int64_t row = w.map[i];
+    const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts);
+    const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
+    if (part == 0 && threadIdx.x < 32) {
+        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
+        double sum = 0.0;
+        if (k == 0) {
+            sum = l - (double)z[labels[row]];
+        } else {
+            for (int j = threadIdx.x; j < k; j += 32) {
+                const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
+                if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            sum *= (double)temp * (double)temp;
+        }
+        if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
+    }
+    while (col < hi) {
+        float e[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) e[x] = col + x < V ? scale * ex2(__fmaf_rn(f[x], c2, -ms.x)) : 0.0f;
+        const int at = col;
+        col += kRowCols;
+        if (col < hi) load8_rw(z + col, f);
+        uint32_t o[TERMS][4];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             __nv_bfloat16 t[TERMS], u[TERMS];
+            split_terms<TERMS>(e[j], t); split_terms<TERMS>(e[j + 1], u);
 #pragma unroll
-            for (int x = j; x < j + 2; ++x) f[x] = (i < count && col + x < V) ? rc.y * ex2(__fmaf_rn(f[x], c2, -rc.x)) : 0.0f;
-            split_terms<TERMS>(f[j], t); split_terms<TERMS>(f[j + 1], u);
-#pragma unroll
-            for (int p = 0; p < TERMS; ++p) e[p][j / 2] = pack2(t[p], u[p]);
+            for (int p = 0; p < TERMS; ++p) o[p][j / 2] = pack2(t[p], u[p]);
         }
 #pragma unroll
-        for (int p = 0; p < TERMS; ++p) *reinterpret_cast<uint4*>(g + p * plane + col) = make_uint4(e[p][0], e[p][1], e[p][2], e[p][3]);
+        for (int p = 0; p < TERMS; ++p) *reinterpret_cast<uint4*>(g + p * plane + at) = make_uint4(o[p][0], o[p][1], o[p][2], o[p][3]);
     }
-    if (i >= count) return;
     __syncthreads();                                       // the targets' entries are written over what the threads above wrote
-    const int64_t lo = (int64_t)cb * kRowCols, hi = lo + kRowCols;
     for (int j = threadIdx.x; j < (k > 0 ? k : 1); j += 256) {
         const int32_t at = k > 0 ? w.eidx[row * k + j] : labels[row];
         if (at == INT32_MAX || at < lo || at >= hi || (j > 0 && w.eidx[row * k + j - 1] == at)) continue;
-        float x = rc.y * ex2(__fmaf_rn(z[at], c2, -rc.x));
-        if (k == 0) x -= rc.z;
-        else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * rc.z;
+        float x = scale * ex2(__fmaf_rn(z[at], c2, -ms.x));
+        if (k == 0) x -= wt;
+        else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * wt;
         __nv_bfloat16 t[TERMS];
         split_terms<TERMS>(x, t);
 #pragma unroll
@@ -472,32 +504,280 @@ __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int64_t V, int 
     }
 }
 
-// grad_h = the splits' sums in a fixed order, rounded once.  A thread takes four columns of a row.
+// grad_h = the splits' sums, rounded once.  A block takes 128 columns of a row; its eight warps add every eighth split, then the
+// eight sums are added: a fixed order.
 template <bool F32>
-__global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int d, float scale, void* __restrict__ out, int64_t ld)
+__global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int n, int d, float scale, void* __restrict__ out, int64_t ld)
 {
     pdl_prologue();
-    const int count = w.ctrl->count, per_row = (d + 3) / 4;
-    const float alpha = scale != 0.0f ? scale / (float)max(count, 1) : 1.0f;
+    __shared__ float4 s_sum[8][32];
+    const int count = w.ctrl->count, per_row = (d + 127) / 128, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int i = blockIdx.x / per_row, j = (blockIdx.x % per_row) * 128 + lane * 4;
+    if (i >= (w.few ? n : count)) return;
     const int64_t plane = w.n_pad * w.dq;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < (int64_t)count * per_row; t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / per_row; const int j = (int)(t % per_row) * 4;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (j < d) {
         const float* p = w.dh + i * w.dq + j;
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-        for (int q = 0; q < w.splits; ++q) {
+        for (int q = warp; q < w.splits; q += 8) {
             const float4 x = *reinterpret_cast<const float4*>(p + q * plane);
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
-        const float v[4] = {s.x * alpha, s.y * alpha, s.z * alpha, s.w * alpha};
-        const int64_t at = (int64_t)w.map[i] * ld + j;
+    }
+    s_sum[warp][lane] = s;
+    __syncthreads();
+    if (warp > 0 || j >= d) return;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (j + c < d) {
-                if (F32) static_cast<float*>(out)[at + c] = v[c];
-                else static_cast<__nv_bfloat16*>(out)[at + c] = __float2bfloat16_rn(v[c]);
+    for (int q = 1; q < 8; ++q) {
+        const float4 x = s_sum[q][lane];
+        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    const float alpha = scale != 0.0f ? scale / (float)max(count, 1) : 1.0f;
+    const bool none = w.few && !(w.ctrl->mask >> i & 1);             // a row without a target: zeros, whatever w holds
+    const float v[4] = {s.x * alpha, s.y * alpha, s.z * alpha, s.w * alpha};
+    const int64_t at = (w.few ? i : w.map[i]) * ld + j;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        if (j + c < d) {
+            const float x = none ? 0.0f : v[c];
+            if (F32) static_cast<float*>(out)[at + c] = x;
+            else static_cast<__nv_bfloat16*>(out)[at + c] = __float2bfloat16_rn(x);
+        }
+    }
+}
+
+// ---- few rows of fp32: products on the CUDA cores ------------------------------------------------------------------------------
+
+// Up to eight rows of fp32: such calls are bound by reading w, which these kernels read as it is; the tensor cores would need its
+// bf16 terms first (10 more bytes a value) and take six products of them (1 x 2048 x 50001: loss 75 us against 393, gradient 243
+// against 726; 8 x 64 x 100: 8 and 16 us against 15 and 23).  bf16 weights feed the tensor cores without a copy, which is faster at any
+// size (1 x 2048 x 50001: 54 us).  Everything is fp32, g too.  No compact copy of the rows: one without a target counts as zeros.
+
+struct Few { const float *h, *w; int64_t ld_h, ld_w; int n, d; int64_t V; const int32_t* tgt; bool vec_h, vec_w; };
+
+// Which rows have a target, one bit each.
+__device__ __forceinline__ uint32_t few_mask(const Few& q)
+{
+    const int lane = threadIdx.x & 31;
+    const int32_t t = lane < q.n ? q.tgt[lane] : -1;
+    return __ballot_sync(0xFFFFFFFFu, t >= 0 && t < q.V);
+}
+
+// Values k .. k + 3 of a row; zeros from `d` on.  The weights pass the L1 by.
+__device__ __forceinline__ float4 few_load(const float* p, int k, int d, bool vec)
+{
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (vec && k + 4 <= d) {
+        asm("ld.global.nc.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p + k));
+    } else {
+        if (k < d) x.x = __ldg(p + k);
+        if (k + 1 < d) x.y = __ldg(p + k + 1);
+        if (k + 2 < d) x.z = __ldg(p + k + 2);
+        if (k + 3 < d) x.w = __ldg(p + k + 3);
+    }
+    return x;
+}
+
+// Adds each of N values over the warp's lanes by halving: in every step a lane passes on the half that it does not keep.  Lane l
+// ends with value l >> (5 - log2 N) in v[0].
+template <int N>
+__device__ __forceinline__ void warp_transpose_sum(float (&v)[N], int lane)
+{
+    int cnt = N;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (cnt > 1) {
+            cnt /= 2;
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) {
+                if (j < cnt) {
+                    const bool hi = lane & o;
+                    const float give = hi ? v[j] : v[j + cnt], keep = hi ? v[j + cnt] : v[j];
+                    v[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, o);
+                }
+            }
+        } else {
+            v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
+        }
+    }
+}
+
+// Logits of NR rows, CW classes to a warp, K over the lanes in 16-byte loads, h in shared memory 1024 columns at a time; (max, sum) per
+// row and block.  Block 0 opens the call: the status, the number of rows with a target, the others' zero results.
+template <int NR>
+__global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, float c2, float* __restrict__ loss, float* __restrict__ lse, Work w)
+{
+    pdl_prologue();
+    constexpr int CW = NR == 8 ? 4 : 8, N = NR * CW, SHIFT = N == 32 ? 0 : 1, KC = 1024;
+    __shared__ float4 s_h[NR][KC / 4];
+    __shared__ float2 s_part[8][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t mask = few_mask(q);
+    if (blockIdx.x == 0 && threadIdx.x < 32) {
+        if (lane == 0) { w.ctrl->status = DQ_OK; w.ctrl->count = __popc(mask); w.ctrl->mask = mask; }
+        if (lane < q.n && !(mask >> lane & 1)) { loss[lane] = 0.0f; if (lse) lse[lane] = 0.0f; }
+    }
+    const int idx = lane >> SHIFT, r = idx / CW, c = idx % CW;             // the value a lane ends with
+    float m = -INFINITY, s = 0.0f;
+    int held = -1;                                                         // columns of h in shared memory start here
+    for (int64_t b = (int64_t)blockIdx.x * 8 * CW; b < q.V; b += (int64_t)gridDim.x * 8 * CW) {
+        const int64_t v = b + warp * CW;
+        float acc[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+        for (int k0 = 0; k0 < q.d; k0 += KC) {
+            if (held != k0) {
+                if (held >= 0) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    const int k = k0 + threadIdx.x * 4;
+                    s_h[i][threadIdx.x] = mask >> i & 1 ? few_load(q.h + i * q.ld_h, k, q.d, q.vec_h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+                held = k0;
+                __syncthreads();
+            }
+            const int kn = min(KC, q.d - k0);
+#pragma unroll 2
+            for (int k = lane * 4; k < kn; k += 128) {
+                float4 y[CW];
+#pragma unroll
+                for (int j = 0; j < CW; ++j) y[j] = few_load(q.w + min(v + j, q.V - 1) * q.ld_w, k0 + k, q.d, q.vec_w);
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    const float4 x = s_h[i][k >> 2];
+#pragma unroll
+                    for (int j = 0; j < CW; ++j) {
+                        float& t = acc[i * CW + j];
+                        t = __fmaf_rn(x.x, y[j].x, t); t = __fmaf_rn(x.y, y[j].y, t); t = __fmaf_rn(x.z, y[j].z, t); t = __fmaf_rn(x.w, y[j].w, t);
+                    }
+                }
             }
         }
+        warp_transpose_sum<N>(acc, lane);
+        if (v + c < q.V) {
+            const float t = acc[0] * c2, nm = fmaxf(m, t), use = nm == -INFINITY ? 0.0f : nm;
+            if ((lane & SHIFT) == 0 && (mask >> r & 1)) w.z[(int64_t)r * w.vc + v + c] = acc[0];
+            s = s * ex2(m - use) + ex2(__fmaf_rn(acc[0], c2, -use));
+            m = nm;
+        }
+    }
+    s_part[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x < NR) {
+        m = -INFINITY; s = 0.0f;
+        for (int i = 0; i < 8; ++i)
+            for (int j = 0; j < CW; ++j) {
+                const float2 p = s_part[i][(threadIdx.x * CW + j) << SHIFT];
+                const float nm = fmaxf(m, p.x), use = nm == -INFINITY ? 0.0f : nm;
+                s = s * exp2f(m - use) + p.y * exp2f(p.x - use);
+                m = nm;
+            }
+        w.part[(int64_t)threadIdx.x * w.parts + blockIdx.x] = make_float2(m, s);
+    }
+}
+
+// lse and loss, and g [classes][NR] as fp32 where it is wanted; a block takes part of a row's columns.
+template <int NR>
+__global__ void __launch_bounds__(256) vocab_few_rows_kernel(Work w, int n, int V, int k, int parts_per_row, bool grad, const int32_t* __restrict__ labels,
+                                                             const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+                                                             float* __restrict__ lse)
+{
+    pdl_prologue();
+    const int row = blockIdx.x / parts_per_row, part = blockIdx.x % parts_per_row, span = (V + parts_per_row - 1) / parts_per_row;
+    const int lo = part * span, hi = min(V, lo + span);
+    if (row >= n || !(w.ctrl->mask >> row & 1)) {
+        if (grad) for (int col = lo + threadIdx.x; col < hi; col += 256) w.gf[(int64_t)col * NR + row] = 0.0f;
+        return;
+    }
+    const float* const z = w.z + (int64_t)row * w.vc;
+    const float2 ms = block_join(w.part + (int64_t)row * w.parts, w.parts);
+    const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
+    if (part == 0 && threadIdx.x < 32) {
+        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
+        double sum = 0.0;
+        if (k == 0) {
+            sum = l - (double)z[labels[row]];
+        } else {
+            for (int j = threadIdx.x; j < k; j += 32) {
+                const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
+                if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            sum *= (double)temp * (double)temp;
+        }
+        if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
+    }
+    if (!grad) return;
+#pragma unroll 4
+    for (int col = lo + threadIdx.x; col < hi; col += 256) w.gf[(int64_t)col * NR + row] = scale * ex2(__fmaf_rn(z[col], c2, -ms.x));
+    __syncthreads();                                       // the targets' entries are written over what the threads above wrote
+    for (int j = threadIdx.x; j < (k > 0 ? k : 1); j += 256) {
+        const int32_t at = k > 0 ? w.eidx[row * k + j] : labels[row];
+        if (at == INT32_MAX || at < lo || at >= hi || (j > 0 && w.eidx[row * k + j - 1] == at)) continue;
+        float x = scale * ex2(__fmaf_rn(z[at], c2, -ms.x));
+        if (k == 0) x -= wt;
+        else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * wt;
+        w.gf[(int64_t)at * NR + row] = x;
+    }
+}
+
+// Both gradients.  A block takes 128 columns and a range of classes, its warps every eighth class: a lane keeps its four columns of h and of
+// its share of grad_h in registers, reads four values of w and writes four of grad_w per class.
+template <int NR>
+__global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(const Few q, float scale, float* __restrict__ gw, int64_t ld_gw, bool vec_gw, int chunks,
+                                                              int64_t span, Work w)
+{
+    pdl_prologue();
+    __shared__ float4 s_sum[8][NR][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = (blockIdx.x % chunks) * 128 + lane * 4, range = blockIdx.x / chunks;
+    const int64_t v0 = range * span, v1 = min(q.V, v0 + span);
+    const uint32_t mask = w.ctrl->mask;
+    const float alpha = scale != 0.0f ? scale / (float)max(w.ctrl->count, 1) : 1.0f;
+    float4 h[NR], acc[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        h[i] = mask >> i & 1 ? few_load(q.h + i * q.ld_h, k, q.d, q.vec_h) : acc[i];
+    }
+    if (k < q.d) {
+#pragma unroll 8
+        for (int64_t v = v0 + warp; v < v1; v += 8) {
+            const float4 y = few_load(q.w + v * q.ld_w, k, q.d, q.vec_w);
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < NR; i += 2) {
+                const float2 g = __ldg(reinterpret_cast<const float2*>(w.gf + v * NR + i));
+                o.x = __fmaf_rn(g.y, h[i + 1].x, __fmaf_rn(g.x, h[i].x, o.x)); o.y = __fmaf_rn(g.y, h[i + 1].y, __fmaf_rn(g.x, h[i].y, o.y));
+                o.z = __fmaf_rn(g.y, h[i + 1].z, __fmaf_rn(g.x, h[i].z, o.z)); o.w = __fmaf_rn(g.y, h[i + 1].w, __fmaf_rn(g.x, h[i].w, o.w));
+                acc[i].x = __fmaf_rn(g.x, y.x, acc[i].x); acc[i].y = __fmaf_rn(g.x, y.y, acc[i].y);
+                acc[i].z = __fmaf_rn(g.x, y.z, acc[i].z); acc[i].w = __fmaf_rn(g.x, y.w, acc[i].w);
+                acc[i + 1].x = __fmaf_rn(g.y, y.x, acc[i + 1].x); acc[i + 1].y = __fmaf_rn(g.y, y.y, acc[i + 1].y);
+                acc[i + 1].z = __fmaf_rn(g.y, y.z, acc[i + 1].z); acc[i + 1].w = __fmaf_rn(g.y, y.w, acc[i + 1].w);
+            }
+            float* const out = gw + v * ld_gw + k;
+            o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+            if (vec_gw && k + 4 <= q.d) {
+                *reinterpret_cast<float4*>(out) = o;
+            } else {
+                out[0] = o.x;
+                if (k + 1 < q.d) out[1] = o.y;
+                if (k + 2 < q.d) out[2] = o.z;
+                if (k + 3 < q.d) out[3] = o.w;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NR; ++i) s_sum[warp][i][lane] = acc[i];
+    __syncthreads();
+    if (warp < NR && warp < q.n && k < q.d) {
+        float4 s = s_sum[0][warp][lane];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            const float4 x = s_sum[i][warp][lane];
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        *reinterpret_cast<float4*>(w.dh + ((int64_t)range * w.n_pad + warp) * w.dq + k) = s;
     }
 }
 
@@ -1024,9 +1304,33 @@ int row_alignment(const void* p, int64_t row_bytes)
     return ptr_aligned(p, 32) && row_bytes % 32 == 0 ? 2 : 1;
 }
 
+template <int NR>
+int run_few(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, cudaStream_t st)
+{
+    const int d = (int)v->d, k = v->k, n = (int)v->n, V = (int)v->V;
+    const float c2 = (float)(1.4426950408889634 / (double)t.temp);
+    bool ok = true;
+    if (k > 0)
+        ok = launch_k(vocab_targets_kernel<true>, dim3(1), dim3(256), 0, st, t.top_idx, t.top_logits, t.teacher_lse, 1.0f / t.temp, (int64_t)n, k, v->V,
+                      Weights{nullptr, 0, 0, 0, 0, 1}, w) == cudaSuccess;
+    const Few q = {static_cast<const float*>(v->h), static_cast<const float*>(v->w), v->ld_h, v->ld_w, n, d, v->V, k > 0 ? w.tgt : t.labels,
+                   row_alignment(v->h, v->ld_h * 4) > 0, row_alignment(v->w, v->ld_w * 4) > 0};
+    ok = ok && launch_k(vocab_few_logits_kernel<NR>, dim3((unsigned)w.parts), dim3(256), 0, st, q, c2, loss, lse, w) == cudaSuccess;
+    const int parts_per_row = g ? (int)min((int64_t)32, (v->V + 1023) / 1024) : 1;
+    ok = ok && launch_k(vocab_few_rows_kernel<NR>, dim3((unsigned)((g ? NR : n) * parts_per_row)), dim3(256), 0, st, w, n, V, k, parts_per_row, g != nullptr, t.labels,
+                        g ? g->weight : (const float*)nullptr, t.temp, c2, loss, lse) == cudaSuccess;
+    if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
+    const float scale = g->weight ? 0.0f : t.temp;
+    ok = ok && launch_k(vocab_few_grads_kernel<NR>, dim3((unsigned)(w.chunks * w.splits)), dim3(256), 0, st, q, scale, static_cast<float*>(g->gw), g->ld_w,
+                        row_alignment(g->gw, g->ld_w * 4) > 0, w.chunks, w.span, w) == cudaSuccess;
+    ok = ok && launch_k(vocab_grad_h_kernel<true>, dim3((unsigned)(n * ((d + 127) / 128))), dim3(256), 0, st, w, n, d, scale, g->gh, g->ld_h) == cudaSuccess;
+    return ok ? DQ_OK : DQ_ERR_CUDA;
+}
+
 template <bool F32>
 int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
 {
+    if (w.few) return w.few == 2 ? run_few<2>(v, t, loss, lse, g, w, st) : run_few<8>(v, t, loss, lse, g, w, st);
     const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2;
     const int64_t n = v->n, V = v->V;
     const int blocks = dev.sms * 8;
@@ -1062,8 +1366,9 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
         // cheaper than forming them again (2 d flops, six times that for fp32) and merges the join with what follows it.
         ok = ok && launch_mma<kLogits, F32>(n, w.logits, m, a, w, dev, st);
-        const int per_row = (int)((w.vc + kRowCols - 1) / kRowCols);
-        ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(up(n, kTileK) * per_row)), dim3(256), 0, st, w, V, k, per_row, t.labels, weight, t.temp, a.c2,
+        const int64_t rows = up(n, kTileK);
+        const int per_row = (int)min((w.vc + kRowCols - 1) / kRowCols, (4 * dev.sms + n - 1) / n);      // some blocks for every SM
+        ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, w, (int)V, k, per_row, t.labels, weight, t.temp, a.c2,
                             loss, lse) == cudaSuccess;
     } else {
         ok = ok && launch_mma<kLse, F32>(n, w.logits, m, a, w, dev, st);
@@ -1092,10 +1397,8 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         if (a.align_w) ok = ok && make_out_map(&u.m[4], F32, static_cast<char*>(g->gw) + v0 * g->ld_w * elem, d, vn, g->ld_w);
         ok = ok && make_map(&u.m[1], wv, d, vn, wpitch, T, V * wpitch, kTileK) && launch_mma<kGrads, F32>(n, w.grads, u, a, w, dev, st);
     }
-    if (w.splits > 1) {
-        const int64_t need = (n * ((d + 3) / 4) + 255) / 256;
-        ok = ok && launch_k(vocab_grad_h_kernel<F32>, dim3((unsigned)min((int64_t)blocks, need)), dim3(256), 0, st, w, d, a.scale, g->gh, g->ld_h) == cudaSuccess;
-    }
+    if (w.splits > 1)
+        ok = ok && launch_k(vocab_grad_h_kernel<F32>, dim3((unsigned)(n * ((d + 127) / 128))), dim3(256), 0, st, w, (int)n, d, a.scale, g->gh, g->ld_h) == cudaSuccess;
     return ok ? DQ_OK : DQ_ERR_CUDA;
 }
 
@@ -1156,8 +1459,8 @@ int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
         const int64_t bytes = carve(&u, grad != 0, dev.sms).bytes;
         if (bytes > most) most = bytes;
     };
-    for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128
-    see(v->n);
+    for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128, but for few rows
+    see(v->n); see(2); see(kFewRows);
     return most;
 }
 
