@@ -170,6 +170,11 @@ __device__ __forceinline__ uint32_t pack2(__nv_bfloat16 lo, __nv_bfloat16 hi)
 {
     return (uint32_t)__bfloat16_as_ushort(lo) | ((uint32_t)__bfloat16_as_ushort(hi) << 16);
 }
+__device__ __forceinline__ uint32_t round2(float lo, float hi)          // both to bf16 in one instruction
+{
+    const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
 
 // Values j..j+7 of a row of `d` to their bf16 terms, zeros behind the row's end.
 template <bool F32>
@@ -848,6 +853,7 @@ __device__ __forceinline__ void store_terms(__nv_bfloat16* dst, int64_t plane, c
     uint32_t e[TERMS][8];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
+        if (TERMS == 1) { e[0][i / 2] = round2(f[i], f[i + 1]); continue; }
         __nv_bfloat16 t[TERMS], u[TERMS];
         split_terms<TERMS>(f[i], t);
         split_terms<TERMS>(f[i + 1], u);
@@ -1026,26 +1032,31 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         float* const stage = staging + (warp - 4) * kPiece * 32 + lane;       // [column][lane]
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        // out by TMA: the row goes to shared memory in pieces of 128 bytes (128-byte swizzle, two buffers in turn), one lane sends 32
-        // rows of it.  Stores straight from registers cost the L1 a pass for each row (64 x 2048 x 65536: 155 us against 1xx)
+        // Out by TMA: 32 rows of two pieces of 128 bytes go to shared memory (128-byte swizzle), one lane sends them.
         char* const obuf = tail + (warp - 4) * 8192;
-        int turn = 0;
-        auto send = [&](const float* f, bool f32, int x, int y) {
-            if (lane == 0) tma_store_wait_read<1>();
+        auto send = [&](const float* f, bool f32, int x, int y, int have) {
+            const int step = f32 ? 32 : 64;                               // columns of a piece
+            if (lane == 0) tma_store_wait_read();
             __syncwarp();
-            char* const row = obuf + turn * 4096 + lane * 128;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                uint4 v;
-                if (f32) v = make_uint4(__float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]), __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
-                else v = make_uint4(pack2(__float2bfloat16_rn(f[8 * c]), __float2bfloat16_rn(f[8 * c + 1])), pack2(__float2bfloat16_rn(f[8 * c + 2]), __float2bfloat16_rn(f[8 * c + 3])),
-                                    pack2(__float2bfloat16_rn(f[8 * c + 4]), __float2bfloat16_rn(f[8 * c + 5])), pack2(__float2bfloat16_rn(f[8 * c + 6]), __float2bfloat16_rn(f[8 * c + 7])));
-                *reinterpret_cast<uint4*>(row + ((c ^ (lane & 7)) << 4)) = v;
+            for (int q = 0; q < 2; ++q) {
+                char* const row = obuf + q * 4096 + lane * 128;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float* e = f + q * step + c * step / 8;
+                    uint4 v;
+                    if (f32) v = make_uint4(__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
+                    else v = make_uint4(round2(e[0], e[1]), round2(e[2], e[3]), round2(e[4], e[5]), round2(e[6], e[7]));
+                    *reinterpret_cast<uint4*>(row + ((c ^ (lane & 7)) << 4)) = v;
+                }
             }
             fence_async_shared();
             __syncwarp();
-            if (lane == 0) tma_store(&mo, smem_u32(obuf + turn * 4096), x, y);
-            turn ^= 1;
+            if (lane == 0) {
+                tma_store(&mo, smem_u32(obuf), x, y);
+                if (step < have) tma_store(&mo, smem_u32(obuf) + 4096, x + step, y);
+                tma_store_commit();
+            }
         };
         const float alpha = a.scale != 0.0f ? a.scale / (float)max(count, 1) : 1.0f;
         int acc = 0; uint32_t aph = 0; bool ok = true;
@@ -1067,21 +1078,29 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 if (KIND == kProb) rc = w.rowc[r];
             }
             float f[kHalf];
-#pragma unroll
-            for (int j = 0; j < kHalf; ++j) f[j] = 0.0f;
             const int steps = (q.k1 - q.k0) * a.pairs;
+            if (steps <= 0) {
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) f[j] = 0.0f;
+            }
             for (int i0 = 0; i0 < steps; i0 += kSegment) {
                 __syncwarp();
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(tfull(acc), aph, gave_up))) { ok = false; break; }    // the warp leaves as one
                 fence_after_sync();
                 const uint32_t d = tmem + lanes + acc * TN + half * kHalf;
+                if (i0 == 0) {
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(d + c, v);
+                    for (int c = 0; c < kHalf; c += 32) tmem_ld32(d + c, reinterpret_cast<uint32_t (&)[32]>(f[c]));
                     tmem_wait_ld();
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[c + j] += __uint_as_float(v[j]);
+                    for (int c = 0; c < kHalf; c += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(d + c, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[c + j] += __uint_as_float(v[j]);
+                    }
                 }
                 fence_before_sync();
                 __syncwarp();
@@ -1095,7 +1114,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 for (int c = 0; c < kHalf; c += kPiece) {
                     if (S::kTmaOut) {
                         // (rows behind the last one hold nothing that is read; they stay inside n_pad)
-                        if (c % 32 == 0 && c < have) send(f + c, true, col + c, r - lane);
+                        if (c % 64 == 0 && c < have) send(f + c, true, col + c, r - lane, have - c);
                     } else if (KIND == kLogits) {
                         if (r < count && c < have) {
                             float* o = w.z + (int64_t)r * w.vc + col + c;
@@ -1179,8 +1198,8 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 }
                 if (S::kTmaOut && is_w && a.align_w) {
 #pragma unroll
-                    for (int c = 0; c < kHalf; c += F32 ? 32 : 64)
-                        if (c < have && r - lane < a.kdim) send(f + c, F32, col + c, r - lane);
+                    for (int c = 0; c < kHalf; c += F32 ? 64 : 128)
+                        if (c < have && r - lane < a.kdim) send(f + c, F32, col + c, r - lane, have - c);
                 } else if (out) {
                     const int64_t row = is_w ? a.v0 + r : w.map[r], ld = is_w ? a.ld_gw : a.ld_gh;
                     store_row<F32>(is_w ? a.gw : a.gh, row * ld + col, f, have, is_w ? a.align_w : a.align_h);

@@ -395,8 +395,12 @@ def test_refusals_with_tensors(dq):
     assert dq.dq_distill_loss(layer, labels, loss, None, 1.0, loss, lse) == bad             # k = 0 holder
     with pytest.raises(dq.DqError):
         dq.Vocab(h.t().contiguous().t(), w)._bytes(dq.Vocab._shape(h.t().contiguous().t(), w, 0), True, w.device)
-    tiny = dq.Vocab(h, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
-    assert dq.dq_xent_grad(tiny, labels, None, loss, lse, gh, gw) == dq.DQ_ERR_SHAPE
+    for rows, size in ((16, 128), (400, 4096)):                                            # a workspace too small, for one launch and for several
+        hh = torch.zeros(rows, 32, device="cuda")
+        o = _outputs(hh, w)
+        assert dq.dq_xent_grad(dq.Vocab(hh, w, workspace=torch.empty(size, dtype=torch.uint8, device="cuda")),
+                               torch.zeros(rows, dtype=torch.int32, device="cuda"), None, *o) == dq.DQ_ERR_SHAPE
+        assert all(torch.isnan(x).all() for x in o)
     only_loss = dq.Vocab(h, w, grad=False)
     assert dq.dq_xent_grad(only_loss, labels, None, loss, lse, gh, gw) == dq.DQ_ERR_SHAPE
     assert torch.isnan(loss).all() and torch.isnan(gh).all() and torch.isnan(gw).all()      # nothing was written
