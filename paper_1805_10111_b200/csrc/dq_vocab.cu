@@ -30,14 +30,29 @@ constexpr int kPiece = 16;                                // columns staged at a
 constexpr int kSegment = 8;                               // tiles of K summed in tensor memory before the sum moves to registers
 constexpr int64_t kGradBytes = 256ll << 20;               // bound on the piece of g kept between products
 
+bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
 // Tiles of a product over m rows (of M) and `cols` columns.  128 by 64 where tiles of 256 columns would leave half of the SMs without one:
-// more SMs then share the loads, which is what bounds such products (64 x 512 x 2000: xx us against yy).  Otherwise 256 columns, shared by a
-// pair of CTAs unless one CTA's 128 rows hold them all.
+// more SMs then share the loads, which is what bounds such products (64 x 1024 x 2000 gradient 25 us against 30, fp32 44 against 63).
+// Otherwise 256 columns, shared by a pair of CTAs unless one CTA's 128 rows hold them all.
 struct Shape { int tn, cg; };
 Shape tile_shape(int64_t n, int64_t m, int64_t cols, int sms)
 {
     if ((m + 127) / 128 * ((cols + kTileN - 1) / kTileN) < sms / 2) return {kNarrow, 1};
     return {kTileN, n > 128 ? 2 : 1};
+}
+
+// The logits' tiles of up to 128 rows cost what reading their rows of w costs: of a width that gives every SM the same number of them
+// (128 to 256 columns, a multiple of 32; 1 x 2048 x 50001: xx us against yy at 256).
+Shape logit_shape(int64_t n, int64_t V, int sms)
+{
+    Shape s = tile_shape(n, n, V, sms);
+    if (n <= 128 && s.tn == kTileN) {
+        const int64_t rounds = (V + (int64_t)kTileN * sms - 1) / ((int64_t)kTileN * sms);
+        s.tn = (int)up((V + rounds * sms - 1) / (rounds * sms), 32);
+    }
+    return s;
 }
 
 struct Ctrl { int status; int count; uint32_t mask; };    // head of the workspace: status, rows with a target, which (few rows)
@@ -64,8 +79,6 @@ struct Work {
     int64_t bytes;
 };
 
-bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
 __host__ __device__ constexpr int few_blocks(int rows) { return rows == 2 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
@@ -78,7 +91,7 @@ Work carve(const dq_vocab* v, bool grad, int sms)
     const bool few = f32 && v->n >= 1 && v->n <= kFewRows;
     w.n_pad = few ? kFewRows : up(v->n > 0 ? v->n : 1, 256);
     w.dp = up(v->d, 8); w.dq = up(v->d, 8);
-    w.logits = tile_shape(v->n, v->n, v->V, sms);
+    w.logits = logit_shape(v->n, v->V, sms);
     w.parts = 2 * (int)((v->V + w.logits.tn - 1) / w.logits.tn);
     w.direct_w = !f32 && ptr_aligned(v->w, 16) && v->ld_w % 8 == 0;
     const int k = v->k > 0 ? v->k : 1;
@@ -792,6 +805,7 @@ struct MmaArgs {
     int cols;                // extent of the tile's N axis: classes of the piece, or d (kGrads)
     int kdim;                // extent of the summed axis: d, or classes of the piece (grad_h; grad_w sums over the rows with a target)
     int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
+    int tn;                  // columns of a tile of the logits (kLse, kLogits)
     int v0;                  // first class of the piece
     int k;                   // targets per row (0: one label)
     float c2;                // log2(e) / T
@@ -911,6 +925,8 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
     using S = Smem<CG, KIND, TN>;
     constexpr int NS = S::kStages, SB = S::kStage, BN = TN / CG, kHalf = TN / 2;
     constexpr bool GRADS = KIND == kGrads;
+    // columns of a tile: TN, or fewer where few rows make the time that of reading w (see tile_shape)
+    const int tn = CG == 1 && TN == kTileN && (KIND == kLse || KIND == kLogits) ? a.tn : TN;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
     float* const staging = reinterpret_cast<float*>(tail);
@@ -945,7 +961,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
 
     // Tiles: those whose rows are the rows with a target (kGrads: grad_h, times splits), then grad_w's, shorter ones last.
     const int count = w.ctrl->count;
-    const int nt = (a.cols + TN - 1) / TN, mt = (count + 128 * CG - 1) / (128 * CG), kit = (a.kdim + kTileK - 1) / kTileK;
+    const int nt = (a.cols + tn - 1) / tn, mt = (count + 128 * CG - 1) / (128 * CG), kit = (a.kdim + kTileK - 1) / kTileK;
     const int mt_w = (a.kdim + 128 * CG - 1) / (128 * CG), kit_w = (count + kTileK - 1) / kTileK;
     const int tiles_h = mt * nt * (GRADS ? a.splits : 1), tiles = tiles_h + (GRADS ? mt_w * nt : 0);
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -960,13 +976,13 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
-                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * TN + (int)rank * BN;
+                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * tn + (int)rank * BN;
                 for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
                     const int za = term_a(p), zb = term_b(p);
                     for (int kb = q.k0; kb < q.k1; ++kb) {
                         if (!mbar_wait(empty(s), ph ^ 1u, gave_up)) { ok = false; break; }
                         const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
-                        if (rank == 0) mbar_expect_tx(full(s), CG * SB);
+                        if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) * 128));
                         const int x = kb * kTileK;
                         if (is_w) {
                             tma_load<CG>(&mc, dst, bar, ym, x, za);
@@ -999,7 +1015,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
                 // bytes from one K of 16 to the next, and between blocks of 64 of an operand that lies across (see smem_desc)
-                const uint32_t idesc = instr_desc_bf16(128 * CG, TN, is_w, GRADS), a_step = (is_w ? 16 * 128 : 32) >> 4;
+                const uint32_t idesc = instr_desc_bf16(128 * CG, tn, is_w, GRADS), a_step = (is_w ? 16 * 128 : 32) >> 4;
                 constexpr uint32_t b_step = (GRADS ? 16 * 128 : 32) >> 4;
                 const int steps = (q.k1 - q.k0) * a.pairs;
                 for (int i0 = 0; i0 < steps && ok; i0 += kSegment) {
@@ -1064,8 +1080,8 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             const Tile q = tile(t);
             const bool is_w = GRADS && t >= tiles_h;
             const int r = q.m * 128 * CG + (int)rank * 128 + quarter * 32 + lane;     // the thread's row of the tile's M axis
-            const int col = q.n * TN + half * kHalf;                                  // its first column
-            const int have = a.cols - col;                                            // columns that exist
+            const int col = q.n * tn + half * kHalf;                                  // its first column
+            const int have = min(a.cols - col, tn - half * kHalf);                    // columns that exist
             // targets of the row: the first one not before the half tile
             int64_t e0 = 0; int pos = 0, next = INT32_MAX; const int ke = a.k > 0 ? a.k : 1, v_at = a.v0 + col;
             float4 rc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1123,7 +1139,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                             for (int j = 0; j < 8; ++j) { x[j] = f[c + j]; y[j] = f[c + 8 + j]; }
                             store8(o, x); store8(o + 8, y);
                         }
-                    } else if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
+                    } else if (c < have && __any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
 #pragma unroll
                         for (int j = 0; j < kPiece; ++j) stage[j * 32] = f[c + j];
                         while (next < v_at + c + kPiece) {
@@ -1379,7 +1395,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     ok = ok && make_map(&m.m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128) &&
          make_map(&m.m[1], wsrc, d, V, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg);
     if (w.keep) ok = ok && make_out_map(&m.m[4], true, w.z, w.vc, w.n_pad, w.vc);
-    a.cols = (int)V; a.kdim = d;
+    a.cols = (int)V; a.kdim = d; a.tn = w.logits.tn;
     const float* weight = g ? g->weight : nullptr;
     if (w.keep) {
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
@@ -1408,7 +1424,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         a.v0 = (int)v0;
         if (!w.keep) {
             a.cols = vn; a.kdim = d; a.splits = 1;
-            ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg) && launch_mma<kProb, F32>(n, w.logits, m, a, w, dev, st);
+            ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, kTileN / w.logits.cg) && launch_mma<kProb, F32>(n, Shape{kTileN, w.logits.cg}, m, a, w, dev, st);
         }
         a.cols = d; a.kdim = vn; a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
