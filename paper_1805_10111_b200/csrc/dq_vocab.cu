@@ -806,6 +806,7 @@ struct MmaArgs {
     int kdim;                // extent of the summed axis: d, or classes of the piece (grad_h; grad_w sums over the rows with a target)
     int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
     int tn;                  // columns of a tile of the logits (kLse, kLogits)
+    int am;                  // rows in a box of h, and of g for grad_h, where a pair of CTAs does not share the tile
     int v0;                  // first class of the piece
     int k;                   // targets per row (0: one label)
     float c2;                // log2(e) / T
@@ -926,6 +927,8 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
     constexpr int NS = S::kStages, SB = S::kStage, BN = TN / CG, kHalf = TN / 2;
     constexpr bool GRADS = KIND == kGrads;
     // columns of a tile: TN, or fewer where few rows make the time that of reading w (see tile_shape)
+    // Rows that a tile of 128 has to have loaded: the others' results are not looked at, whatever shared memory holds in their place.
+    const int am = CG == 1 ? a.am : 128;
     const int tn = CG == 1 && TN == kTileN && (KIND == kLse || KIND == kLogits) ? a.tn : TN;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
@@ -982,7 +985,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                     for (int kb = q.k0; kb < q.k1; ++kb) {
                         if (!mbar_wait(empty(s), ph ^ 1u, gave_up)) { ok = false; break; }
                         const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
-                        if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) * 128));
+                        if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) * 128 - (is_w ? 0 : (128 - am) * 128)));
                         const int x = kb * kTileK;
                         if (is_w) {
                             tma_load<CG>(&mc, dst, bar, ym, x, za);
@@ -1392,10 +1395,11 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
     a.splits = 1; a.scale = g && !g->weight ? t.temp : 0.0f;
     Maps m = {};
-    ok = ok && make_map(&m.m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, 128) &&
+    auto row_box = [&](const Shape& x) { return x.cg == 2 || n > 120 ? 128 : (int)up(n, 8); };
+    ok = ok && make_map(&m.m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, row_box(w.logits)) &&
          make_map(&m.m[1], wsrc, d, V, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg);
     if (w.keep) ok = ok && make_out_map(&m.m[4], true, w.z, w.vc, w.n_pad, w.vc);
-    a.cols = (int)V; a.kdim = d; a.tn = w.logits.tn;
+    a.cols = (int)V; a.kdim = d; a.tn = w.logits.tn; a.am = row_box(w.logits);
     const float* weight = g ? g->weight : nullptr;
     if (w.keep) {
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
@@ -1414,7 +1418,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
 
     // gradients, a piece of the vocabulary at a time
     Maps u = {};
-    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, 128) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
+    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, row_box(w.grads)) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
          make_map(&u.m[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
     a.gh = g->gh; a.gw = g->gw; a.ld_gh = g->ld_h; a.ld_gw = g->ld_w; a.kps = w.kps;
     a.align_h = row_alignment(g->gh, g->ld_h * elem); a.align_w = row_alignment(g->gw, g->ld_w * elem);
@@ -1423,10 +1427,10 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         const __nv_bfloat16* wv = wsrc + v0 * wpitch;
         a.v0 = (int)v0;
         if (!w.keep) {
-            a.cols = vn; a.kdim = d; a.splits = 1;
+            a.cols = vn; a.kdim = d; a.am = row_box(w.logits); a.splits = 1;
             ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, kTileN / w.logits.cg) && launch_mma<kProb, F32>(n, Shape{kTileN, w.logits.cg}, m, a, w, dev, st);
         }
-        a.cols = d; a.kdim = vn; a.first = v0 == 0; a.last = v0 + w.vc >= V;
+        a.cols = d; a.kdim = vn; a.am = row_box(w.grads); a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
         u.m[4] = u.m[3];                                   // (a valid map, though one for grad_w is not used without alignment)
         if (a.align_w) ok = ok && make_out_map(&u.m[4], F32, static_cast<char*>(g->gw) + v0 * g->ld_w * elem, d, vn, g->ld_w);
