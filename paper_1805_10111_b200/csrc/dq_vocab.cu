@@ -61,13 +61,13 @@ struct Ctrl { int status; int count; uint32_t mask; };    // head of the workspa
 struct Work {
     Ctrl* ctrl;
     int32_t *map, *tgt;            // compact row -> row; distillation: 0 or -1, whether a row has a target
-    float4* rowc;                  // compact row: maximum in log2 units, factor of 2^(z - maximum), factor of q
+    float4* rowc;                  // compact row: largest logit m, factor of exp((z - m) / T), factor of q
     int32_t* eidx; float *eq, *elq, *emass;   // distillation: targets of a row by ascending class, q, log q, sum q
     float* zt;                     // logit at every target
     __nv_bfloat16* hp;             // [terms][n_pad][dp] compact rows of h
     __nv_bfloat16* wp;             // [terms][V][dp] w, where it cannot be read in place
     float* z;                      // [n_pad][vc] the logits, where they are few enough to be kept (see run_loss)
-    float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, log2 units
+    float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, see join_pair
     __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
     float* gf;                     // few rows: the logits' gradient [V][few]
     float* dh;                     // [splits][n_pad][dq] sums of grad_h
@@ -142,7 +142,7 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         w.grads = tile_shape(v->n, w.vc > v->n ? w.vc : v->n, v->d, sms);
         const int cg = w.grads.cg, tn = w.grads.tn, units = sms / cg;
         const int tiles = (int)((v->n + 128 * cg - 1) / (128 * cg) * ((v->d + tn - 1) / tn));
-        const int kit = (int)(w.vc / kTileK);
+        const int kit = (int)(((w.vc < v->V ? w.vc : v->V) + kTileK - 1) / kTileK);    // of the first piece, which fills every split
         int splits = tiles < 1 || tiles >= units ? 1 : units / tiles;
         // at least 512 classes to a split (256 for fp32, which takes six products of each): below that the shares' traffic outweighs
         // the products (64 x 512 x 2000 fp32: 44 us at 256, 50 at 512, 63 at 1024; bf16 26, 27, 28)
@@ -362,85 +362,73 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
     }
 }
 
-// Joins the (max, sum) pairs of a row's tiles to lse, forms the loss and the two factors of the gradient; a warp per row.
-__global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const int32_t* __restrict__ labels, const float* __restrict__ weight,
-                                                         float temp, float c2, float* __restrict__ loss, float* __restrict__ lse)
+// (max, sum) pairs: a set of logits z stands for sum exp(z / T) = s 2^(m c2), m the largest z, c2 = log2(e) / T.  The largest term is exactly 1.
+__device__ __forceinline__ void join_pair(float& m, float& s, float qm, float qs, float c2)
+{
+    const float nm = fmaxf(m, qm), use = nm == -INFINITY ? 0.0f : nm;
+    s = s * exp2f((m - use) * c2) + qs * exp2f((qm - use) * c2);
+    m = nm;
+}
+__device__ __forceinline__ void warp_join(float& m, float& s, float c2)          // symmetric in the lanes: all end with the same pair
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) join_pair(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c2);
+}
+
+// A row's loss, by a warp: zt(j) is the logit at its target j.  lse is formed in double and rounded once; the loss is what fp32 gives for
+// lse - z / T, so that it is the loss of the lse that the caller gets (half a step of lse off at most).
+template <class Z>
+__device__ __forceinline__ void write_loss(const Work& w, int64_t row, int k, float2 ms, float temp, float* loss, float* lse, Z zt)
+{
+    const float l = (float)((double)ms.x / (double)temp + log((double)ms.y));
+    const int lane = threadIdx.x & 31;
+    if (k == 0) {
+        if (lane == 0) loss[row] = l - zt(0);
+    } else {
+        double sum = 0.0;
+        for (int j = lane; j < k; j += 32) {
+            const float q = w.eq[row * k + j];
+            if (w.eidx[row * k + j] != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - (double)(__fdiv_rn(zt(j), temp) - l));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == 0) loss[row] = (float)(sum * (double)temp * (double)temp);
+    }
+    if (lane == 0 && lse) lse[row] = l;
+}
+
+// Joins a row's pairs, forms the loss and the two factors of the gradient; a warp per row.
+__global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+                                                         float* __restrict__ lse)
 {
     pdl_prologue();
     const int lane = threadIdx.x & 31, count = w.ctrl->count;
-    const double back = 1.0 / ((double)temp * (double)c2);
     for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < count; i += gridDim.x * 8) {
         const float2* p = w.part + (int64_t)i * w.parts;
         float m = -INFINITY, s = 0.0f;
-        for (int t = lane; t < w.parts; t += 32) {
-            const float2 q = p[t];
-            const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
-            s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
-            m = nm;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float qm = __shfl_xor_sync(0xFFFFFFFFu, m, o), qs = __shfl_xor_sync(0xFFFFFFFFu, s, o);
-            const float nm = fmaxf(m, qm), use = nm == -INFINITY ? 0.0f : nm;
-            s = s * exp2f(m - use) + qs * exp2f(qm - use);       // symmetric in the two lanes: all lanes end with the same pair
-            m = nm;
-        }
-        // sum exp(c z) = s 2^m.  The epilogue multiplied by fl(log2(e) / T): m goes back through the same factor, in double, so that
-        // the factor's rounding does not reach lse, and the loss is subtracted before it is rounded
-        const double l = (double)m * back + log((double)s);
+        for (int t = lane; t < w.parts; t += 32) join_pair(m, s, p[t].x, p[t].y, c2);
+        warp_join(m, s, c2);
         const int64_t row = w.map[i];
-        double sum = 0.0; float mass = 1.0f;
-        if (k == 0) {
-            sum = l - (double)w.zt[row];
-        } else {
-            for (int j = lane; j < k; j += 32) {
-                const float q = w.eq[row * k + j];
-                if (w.eidx[row * k + j] != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)w.zt[row * k + j] / (double)temp - l));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            sum *= (double)temp * (double)temp;
-            mass = w.emass[row];
-        }
-        if (lane == 0) {
-            loss[row] = (float)sum;
-            if (lse) lse[row] = (float)l;
-            // The mean's factor T / count is left to the end: p - q is rounded to bf16 next, and for the entry that matters most,
-            // p - 1 just inside (-1, 0), the rounding is smallest without it (2^-9 at most, 2^-8 with an unlucky factor)
-            const float wt = weight ? weight[row] * temp : 1.0f;
-            w.rowc[i] = make_float4(m, wt * mass / s, wt, 0.0f);
-        }
+        write_loss(w, row, k, make_float2(m, s), temp, loss, lse, [&](int j) { return w.zt[row * (k > 0 ? k : 1) + j]; });
+        // The mean's factor T / count is left to the end: p - q is rounded to bf16 next, and for the entry that matters most,
+        // p - 1 just inside (-1, 0), the rounding is smallest without it (2^-9 at most, 2^-8 with an unlucky factor)
+        const float wt = weight ? weight[row] * temp : 1.0f;
+        if (lane == 0) w.rowc[i] = make_float4(m, wt * (k > 0 ? w.emass[row] : 1.0f) / s, wt, 0.0f);
     }
 }
 
-// The row's (max, sum) pairs joined, by a whole block of 256 threads; every thread gets them.
-__device__ __forceinline__ float2 block_join(const float2* p, int parts)
+// The row's pairs joined by a whole block of 256 threads; every thread gets the result.
+__device__ __forceinline__ float2 block_join(const float2* p, int parts, float c2)
 {
     __shared__ float2 s_part[8];
     float m = -INFINITY, s = 0.0f;
-    for (int t = threadIdx.x; t < parts; t += 256) {
-        const float2 q = p[t];
-        const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
-        s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
-        m = nm;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float qm = __shfl_xor_sync(0xFFFFFFFFu, m, o), qs = __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        const float nm = fmaxf(m, qm), use = nm == -INFINITY ? 0.0f : nm;
-        s = s * exp2f(m - use) + qs * exp2f(qm - use);
-        m = nm;
-    }
+    for (int t = threadIdx.x; t < parts; t += 256) join_pair(m, s, p[t].x, p[t].y, c2);
+    warp_join(m, s, c2);
     if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = make_float2(m, s);
     __syncthreads();
     m = -INFINITY; s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 q = s_part[i];
-        const float nm = fmaxf(m, q.x), use = nm == -INFINITY ? 0.0f : nm;
-        s = s * exp2f(m - use) + q.y * exp2f(q.x - use);
-        m = nm;
-    }
+    for (int i = 0; i < 8; ++i) join_pair(m, s, s_part[i].x, s_part[i].y, c2);
     return make_float2(m, s);
 }
 
@@ -472,28 +460,14 @@ __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, i
     int col = lo + threadIdx.x * 8;
     if (col < hi) load8_rw(z + col, f);                            // on its way while the pairs are joined
     const int64_t row = w.map[i];
-    const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts);
+    const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts, c2);
     const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
-    if (part == 0 && threadIdx.x < 32) {
-        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
-        double sum = 0.0;
-        if (k == 0) {
-            sum = l - (double)z[labels[row]];
-        } else {
-            for (int j = threadIdx.x; j < k; j += 32) {
-                const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
-                if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            sum *= (double)temp * (double)temp;
-        }
-        if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
-    }
+    if (part == 0 && threadIdx.x < 32)
+        write_loss(w, row, k, ms, temp, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
     while (col < hi) {
         float e[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) e[x] = col + x < V ? scale * ex2(__fmaf_rn(f[x], c2, -ms.x)) : 0.0f;
+        for (int x = 0; x < 8; ++x) e[x] = col + x < V ? scale * ex2((f[x] - ms.x) * c2) : 0.0f;
         const int at = col;
         col += kRowCols;
         if (col < hi) load8_rw(z + col, f);
@@ -512,7 +486,7 @@ __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, i
     for (int j = threadIdx.x; j < (k > 0 ? k : 1); j += 256) {
         const int32_t at = k > 0 ? w.eidx[row * k + j] : labels[row];
         if (at == INT32_MAX || at < lo || at >= hi || (j > 0 && w.eidx[row * k + j - 1] == at)) continue;
-        float x = scale * ex2(__fmaf_rn(z[at], c2, -ms.x));
+        float x = scale * ex2((z[at] - ms.x) * c2);
         if (k == 0) x -= wt;
         else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * wt;
         __nv_bfloat16 t[TERMS];
@@ -673,10 +647,8 @@ __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, floa
         }
         warp_transpose_sum<N>(acc, lane);
         if (v + c < q.V) {
-            const float t = acc[0] * c2, nm = fmaxf(m, t), use = nm == -INFINITY ? 0.0f : nm;
             if ((lane & SHIFT) == 0 && (mask >> r & 1)) w.z[(int64_t)r * w.vc + v + c] = acc[0];
-            s = s * ex2(m - use) + ex2(__fmaf_rn(acc[0], c2, -use));
-            m = nm;
+            join_pair(m, s, acc[0], 1.0f, c2);
         }
     }
     s_part[warp][lane] = make_float2(m, s);
@@ -686,9 +658,7 @@ __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, floa
         for (int i = 0; i < 8; ++i)
             for (int j = 0; j < CW; ++j) {
                 const float2 p = s_part[i][(threadIdx.x * CW + j) << SHIFT];
-                const float nm = fmaxf(m, p.x), use = nm == -INFINITY ? 0.0f : nm;
-                s = s * exp2f(m - use) + p.y * exp2f(p.x - use);
-                m = nm;
+                join_pair(m, s, p.x, p.y, c2);
             }
         w.part[(int64_t)threadIdx.x * w.parts + blockIdx.x] = make_float2(m, s);
     }
@@ -708,32 +678,18 @@ __global__ void __launch_bounds__(256) vocab_few_rows_kernel(Work w, int n, int 
         return;
     }
     const float* const z = w.z + (int64_t)row * w.vc;
-    const float2 ms = block_join(w.part + (int64_t)row * w.parts, w.parts);
+    const float2 ms = block_join(w.part + (int64_t)row * w.parts, w.parts, c2);
     const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
-    if (part == 0 && threadIdx.x < 32) {
-        const double l = (double)ms.x / ((double)temp * (double)c2) + log((double)ms.y);      // as in vocab_join_kernel
-        double sum = 0.0;
-        if (k == 0) {
-            sum = l - (double)z[labels[row]];
-        } else {
-            for (int j = threadIdx.x; j < k; j += 32) {
-                const float q = w.eq[row * k + j]; const int32_t at = w.eidx[row * k + j];
-                if (at != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - ((double)z[at] / (double)temp - l));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            sum *= (double)temp * (double)temp;
-        }
-        if (threadIdx.x == 0) { loss[row] = (float)sum; if (lse) lse[row] = (float)l; }
-    }
+    if (part == 0 && threadIdx.x < 32)
+        write_loss(w, row, k, ms, temp, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
     if (!grad) return;
 #pragma unroll 4
-    for (int col = lo + threadIdx.x; col < hi; col += 256) w.gf[(int64_t)col * NR + row] = scale * ex2(__fmaf_rn(z[col], c2, -ms.x));
+    for (int col = lo + threadIdx.x; col < hi; col += 256) w.gf[(int64_t)col * NR + row] = scale * ex2((z[col] - ms.x) * c2);
     __syncthreads();                                       // the targets' entries are written over what the threads above wrote
     for (int j = threadIdx.x; j < (k > 0 ? k : 1); j += 256) {
         const int32_t at = k > 0 ? w.eidx[row * k + j] : labels[row];
         if (at == INT32_MAX || at < lo || at >= hi || (j > 0 && w.eidx[row * k + j - 1] == at)) continue;
-        float x = scale * ex2(__fmaf_rn(z[at], c2, -ms.x));
+        float x = scale * ex2((z[at] - ms.x) * c2);
         if (k == 0) x -= wt;
         else for (int o = j; o < k && w.eidx[row * k + o] == at; ++o) x -= w.eq[row * k + o] * wt;
         w.gf[(int64_t)at * NR + row] = x;
@@ -1158,12 +1114,12 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 float m0 = f[0], m1 = f[1], m2 = f[2], m3 = f[3];
 #pragma unroll
                 for (int j = 4; j < kHalf; j += 4) { m0 = fmaxf(m0, f[j]); m1 = fmaxf(m1, f[j + 1]); m2 = fmaxf(m2, f[j + 2]); m3 = fmaxf(m3, f[j + 3]); }
-                const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * a.c2, off = m == -INFINITY ? 0.0f : m;
+                const float m = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)), off = m == -INFINITY ? 0.0f : m;
                 float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
                 for (int j = 0; j < kHalf; j += 4) {
-                    s0 += ex2(__fmaf_rn(f[j], a.c2, -off)); s1 += ex2(__fmaf_rn(f[j + 1], a.c2, -off));
-                    s2 += ex2(__fmaf_rn(f[j + 2], a.c2, -off)); s3 += ex2(__fmaf_rn(f[j + 3], a.c2, -off));
+                    s0 += ex2((f[j] - off) * a.c2); s1 += ex2((f[j + 1] - off) * a.c2);
+                    s2 += ex2((f[j + 2] - off) * a.c2); s3 += ex2((f[j + 3] - off) * a.c2);
                 }
                 if (r < count) w.part[(int64_t)r * w.parts + 2 * q.n + half] = make_float2(m, (s0 + s1) + (s2 + s3));
             } else if (KIND == kProb) {
@@ -1172,7 +1128,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 for (int c = 0; c < kHalf; c += kPiece) {
 #pragma unroll
                     for (int j = c; j < c + kPiece; ++j)
-                        f[j] = (r < count && j < have) ? rc.y * ex2(__fmaf_rn(f[j], a.c2, -rc.x)) : 0.0f;
+                        f[j] = (r < count && j < have) ? rc.y * ex2((f[j] - rc.x) * a.c2) : 0.0f;
                     if (__any_sync(0xFFFFFFFFu, next < v_at + c + kPiece)) {
 #pragma unroll
                         for (int j = 0; j < kPiece; ++j) stage[j * 32] = f[c + j];
@@ -1411,8 +1367,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
                             loss, lse) == cudaSuccess;
     } else {
         ok = ok && launch_mma<kLse, F32>(n, w.logits, m, a, w, dev, st);
-        ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, t.labels, weight, t.temp, a.c2, loss, lse)
-                       == cudaSuccess;
+        ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, weight, t.temp, a.c2, loss, lse) == cudaSuccess;
     }
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
 

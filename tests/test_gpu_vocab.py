@@ -478,3 +478,25 @@ def test_loss_gradient_as_a_workers_message(dq):
         oracle.master_step(raw, delta, zero, x, eta)
         assert np.array_equal(st.x.cpu().numpy(), x)
     dq.dq_destroy(ctx)
+
+
+@pytest.mark.parametrize("n,d,V", [(1, 1536, 9791), (3, 600, 4161), (130, 520, 2113), (64, 256, 8257)])
+@pytest.mark.parametrize("dt", TYPES)
+def test_split_sums_of_a_ragged_vocabulary(dq, n, d, V, dt):
+    """grad_h's sum over the classes is split where its tiles are few; the last split is short or would be empty."""
+    torch = _torch()
+    _, h, w, labels = _inputs(n, d, V, getattr(torch, dt), n + V)
+    xent_ref(h, w, labels).check(*xent(dq, h, w, labels))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_rows_that_are_sure_of_their_label(dq, dt):
+    """Losses far below lse: the loss is lse - z of the lse that is returned, and stays non-negative where the label leads."""
+    torch = _torch()
+    for n in (2, 200):
+        _, h, w, labels = _inputs(n, 32, 70, getattr(torch, dt), 40 + n)
+        h = (w[labels.long()].float() * 6).to(h.dtype)
+        ref = xent_ref(h, w, labels)
+        loss, lse, gh, gw = xent(dq, h, w, labels)
+        ref.check(loss, lse, gh, gw)
+        assert (loss >= 0).all() and ref.loss.max() < 0.1 * ref.lse.max()
