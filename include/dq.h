@@ -279,11 +279,14 @@ int dq_quantize_pack_static(const float* v, int64_t d, int M, int b, uint64_t se
  *                  the mean.
  * A row without a target (label outside 0..V-1, no present entry) has loss 0, lse 0, a zero row of grad_h and no part in
  * grad_w, whatever its h holds.  A NaN or Inf elsewhere spreads as the formulas say.  Not in place: outputs may not
- * overlap inputs or each other.
+ * overlap inputs or each other.  A row's loss is lse - z / T (times q, summed) of the lse that is returned, as fp32 has
+ * them: off by up to half a step of lse where the two nearly cancel.
  *
  * Types: h, w and the gradients fp32 (DQ_DENSE_F32) or bfloat16 (DQ_DENSE_BF16); everything else fp32 or int32.  Products
  * run on the tensor cores with fp32 accumulation: bfloat16 as it is, with dF/dz rounded to bfloat16 before the gradients'
- * products; fp32 as three bfloat16 terms (24 bits), dF/dz too.  Sums have a fixed order: equal inputs give equal bytes.
+ * products; fp32 as three bfloat16 terms (24 bits), dF/dz too, or, for up to eight rows, on the CUDA cores.  Sums have a
+ * fixed order: equal inputs give equal bytes.  Up to 256 MB of logits stay in the workspace between the two passes over
+ * them; more are formed again, a piece of the vocabulary at a time.
  *
  * The workspace belongs to one call at a time: calls (or captured graphs) whose GPU work may overlap need one each.  No
  * call allocates or synchronises (dq_vocab_status does), so all can be captured.  Launches go to the current device, which
@@ -292,7 +295,7 @@ int dq_quantize_pack_static(const float* v, int64_t d, int M, int b, uint64_t se
 typedef struct {
     int32_t format;            /* DQ_DENSE_F32 or DQ_DENSE_BF16                                             */
     int32_t k;                 /* distillation: entries per row, 1..DQ_VOCAB_MAX_TOP; cross-entropy: 0      */
-    int64_t n, d, V;           /* rows 0..2^24, hidden size 1..2^16, classes 1..2^28                        */
+    int64_t n, d, V;           /* rows 0..2^24, hidden size 1..2^16, classes 1..2^28, n V at most 2^46      */
     const void* h; int64_t ld_h;   /* [n][d], ld_h >= d elements from one row to the next, at most 2^32     */
     const void* w; int64_t ld_w;   /* [V][d].  bfloat16 rows that start on 16 bytes are read in place; others are
                                       copied into the workspace by every call                               */
@@ -310,7 +313,7 @@ int dq_xent_loss(const dq_vocab* v, const int32_t* labels, float* loss, float* l
 int dq_xent_grad(const dq_vocab* v, const int32_t* labels, const float* weight, float* loss, float* lse, void* grad_h, int64_t ld_gh,
                  void* grad_w, int64_t ld_gw, void* stream);
 
-/* top_idx, top_logits [n][k]; teacher_lse [n] or NULL; temperature > 0. */
+/* top_idx, top_logits [n][k]; teacher_lse [n] or NULL; temperature > 0, 1 / temperature finite. */
 int dq_distill_loss(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,
                     float* loss, float* lse, void* stream);
 int dq_distill_grad(const dq_vocab* v, const int32_t* top_idx, const float* top_logits, const float* teacher_lse, float temperature,

@@ -191,8 +191,8 @@ class Vocab:
         self.raw_stream = torch._C._cuda_getCurrentRawStream
         self.c = self._shape(h, w, k)
         self.n, self.d, self.V, self.k = self.c.n, self.c.d, self.c.V, self.c.k
-        if h.device != w.device:
-            raise DqError(DQ_ERR_ARG, "Vocab: h and w are on different devices")
+        if not w.is_cuda or h.device != w.device:
+            raise DqError(DQ_ERR_ARG, "Vocab: h and w are on one CUDA device")
         if workspace is None:
             workspace = torch.empty(self._bytes(self.c, grad, w.device), dtype=torch.uint8, device=w.device)
         elif workspace.device != w.device or not workspace.is_contiguous():

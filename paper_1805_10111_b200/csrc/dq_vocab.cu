@@ -79,7 +79,6 @@ struct Work {
     int64_t bytes;
 };
 
-
 constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
 __host__ __device__ constexpr int few_blocks(int rows) { return rows == 2 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
 
@@ -148,6 +147,8 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         // the products (64 x 512 x 2000 fp32: 44 us at 256, 50 at 512, 63 at 1024; bf16 26, 27, 28)
         const int least = f32 ? 4 : 8;
         if (splits > kit / least) splits = kit / least > 0 ? kit / least : 1;
+        // and none at all where the steps saved cost less than the launch that adds the shares (8 x 256 x 1000: 21 us against 24)
+        if ((kit - kit / splits) * (f32 ? 6 : 1) < 24) splits = 1;
         w.kps = (kit + splits - 1) / splits;
         w.splits = (kit + w.kps - 1) / w.kps;
         if (w.splits > 1 || w.vc < v->V) w.dh = (float*)take(4 * (int64_t)w.splits * w.n_pad * w.dq);
@@ -1396,13 +1397,15 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     return ok ? DQ_OK : DQ_ERR_CUDA;
 }
 
+bool pitch_ok(int64_t ld, int64_t d) { return ld >= d && ld <= (int64_t)1 << 32; }
+
 int check_vocab(const dq_vocab* v)
 {
     if (!v) return DQ_ERR_ARG;
     if (v->format != DQ_DENSE_F32 && v->format != DQ_DENSE_BF16) return DQ_ERR_ARG;
     if (v->n < 0 || v->n > (1 << 24) || v->d < 1 || v->d > (1 << 16) || v->V < 1 || v->V > (1 << 28) || v->k < 0 || v->k > kMaxTop) return DQ_ERR_ARG;
-    if (v->ld_h < v->d || v->ld_w < v->d || v->ld_h > ((int64_t)1 << 32) || v->ld_w > ((int64_t)1 << 32)) return DQ_ERR_ARG;
-    return DQ_OK;
+    if (!pitch_ok(v->ld_h, v->d) || !pitch_ok(v->ld_w, v->d)) return DQ_ERR_ARG;
+    return v->n * v->V <= (int64_t)1 << 46 ? DQ_OK : DQ_ERR_ARG;             // tiles are counted in 32 bits
 }
 
 int run(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, void* stream)
@@ -1414,9 +1417,9 @@ int run(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grad
     if (v->n > 0 && (!v->h || !loss || !ptr_aligned(v->h, elem) || !ptr_aligned(loss, 4) || !ptr_aligned(lse, 4))) return DQ_ERR_ARG;
     if (g) {
         if (!g->gw || (v->n > 0 && !g->gh) || !ptr_aligned(g->gw, elem) || !ptr_aligned(g->gh, elem) || !ptr_aligned(g->weight, 4)) return DQ_ERR_ARG;
-        if (g->ld_h < v->d || g->ld_w < v->d) return DQ_ERR_ARG;
+        if (!pitch_ok(g->ld_h, v->d) || !pitch_ok(g->ld_w, v->d)) return DQ_ERR_ARG;
     }
-    if (!(t.temp > 0.0f) || !isfinite(t.temp)) return DQ_ERR_ARG;
+    if (!(t.temp > 0.0f) || !isfinite(t.temp) || !isfinite(1.5f / t.temp)) return DQ_ERR_ARG;
     Device dev;
     if (!device(&dev)) { cudaGetLastError(); return DQ_ERR_CUDA; }
     const Work w = carve(v, g != nullptr, dev.sms);

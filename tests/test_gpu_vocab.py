@@ -500,3 +500,29 @@ def test_rows_that_are_sure_of_their_label(dq, dt):
         loss, lse, gh, gw = xent(dq, h, w, labels)
         ref.check(loss, lse, gh, gw)
         assert (loss >= 0).all() and ref.loss.max() < 0.1 * ref.lse.max()
+
+
+def test_first_call_of_a_process_can_be_captured(dq):
+    """Nothing that a first call does is out of place in a stream capture (the replayed results are checked in that process)."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_1805_10111_b200 as dq
+for dt, n, V in ((torch.bfloat16, 300, 900), (torch.float32, 5, 400), (torch.float32, 200, 20001)):
+    h, w = torch.randn(n, 64, device="cuda").to(dt), torch.randn(V, 64, device="cuda").to(dt)
+    labels = torch.zeros(n, dtype=torch.int32, device="cuda")
+    layer, out = dq.Vocab(h, w), [torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros_like(h), torch.zeros_like(w)]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        assert dq.dq_xent_grad(layer, labels, None, *out) == 0
+    g.replay(); torch.cuda.synchronize()
+    want = torch.logsumexp(h.double() @ w.double().t(), 1)
+    assert (out[1].double() - want).abs().max() < 1e-4, (out[1], want)
+    assert out[3].abs().max() > 0
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]

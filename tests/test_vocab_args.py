@@ -30,7 +30,7 @@ def _calls(L, v, labels=P, loss=P, lse=P, weight=None, gh=P, ld_gh=16, gw=P, ld_
 
 
 @pytest.mark.parametrize("bad", [dict(format=dq.DQ_CSR_F32), dict(format=7), dict(n=-1), dict(n=(1 << 24) + 1), dict(d=0), dict(d=(1 << 16) + 1),
-                                 dict(V=0), dict(V=(1 << 28) + 1), dict(ld_h=15), dict(ld_w=15), dict(ld_w=-1), dict(ld_h=1 << 40), dict(w=None),
+                                 dict(V=0), dict(V=(1 << 28) + 1), dict(n=1 << 24, V=1 << 24), dict(ld_h=15), dict(ld_w=15), dict(ld_w=-1), dict(ld_h=1 << 40), dict(w=None),
                                  dict(h=None), dict(workspace=None), dict(workspace=P + 16), dict(h=P + 2), dict(w=P + 1)])
 def test_bad_descriptors(L, bad):
     k = {k: v for k, v in bad.items()}
@@ -46,9 +46,9 @@ def test_bad_arguments(L):
     assert _calls(L, _v(k=3), idx=None)[2:] == (dq.DQ_ERR_ARG,) * 2
     assert _calls(L, _v(k=3), t=None)[2:] == (dq.DQ_ERR_ARG,) * 2
     assert _calls(L, _v(), labels=P + 2)[:2] == (dq.DQ_ERR_ARG,) * 2
-    for temp in (0.0, -1.0, float("nan"), float("inf")):
+    for temp in (0.0, -1.0, float("nan"), float("inf"), 1e-39):
         assert _calls(L, _v(k=3), temp=temp)[2:] == (dq.DQ_ERR_ARG,) * 2
-    for kw in (dict(gh=None), dict(gw=None), dict(ld_gh=15), dict(ld_gw=15), dict(gh=P + 2), dict(gw=P + 2), dict(weight=P + 1)):
+    for kw in (dict(gh=None), dict(gw=None), dict(ld_gh=15), dict(ld_gw=15), dict(ld_gh=1 << 40), dict(ld_gw=1 << 40), dict(gh=P + 2), dict(gw=P + 2), dict(weight=P + 1)):
         assert _calls(L, _v(), **kw)[1] == dq.DQ_ERR_ARG
         assert _calls(L, _v(k=3), **kw)[3] == dq.DQ_ERR_ARG
 
@@ -74,6 +74,6 @@ def test_null_descriptor(L):
 def test_holder_refuses_other_types_and_shapes():
     torch = pytest.importorskip("torch")
     h, w = torch.zeros(4, 8), torch.zeros(9, 8)
-    for a, b in ((h.half(), w.half()), (h, w.bfloat16()), (h.double(), w.double()), (h[0], w), (h, w[:, :7])):
+    for a, b in ((h, w), (h.half(), w.half()), (h, w.bfloat16()), (h.double(), w.double()), (h[0], w), (h, w[:, :7])):
         with pytest.raises(dq.DqError):
             dq.Vocab(a, b, workspace=torch.zeros(1 << 20, dtype=torch.uint8))
