@@ -43,14 +43,19 @@ Shape tile_shape(int64_t n, int64_t m, int64_t cols, int sms)
     return {kTileN, n > 128 ? 2 : 1};
 }
 
-// The logits' tiles of up to 128 rows cost what reading their rows of w costs: of a width that gives every SM the same number of them
-// (128 to 256 columns, a multiple of 32; 1 x 2048 x 50001: xx us against yy at 256).
+// Wide tiles of the logits: of the width (a multiple of 32 columns, 128 to 256) that leaves the SMs idle least in the last round, counted as
+// rounds of tiles times their width: both the products and the reading of w go with it (losses: 1 x 2048 x 50001 48 us against 52 at 256
+// columns, 64 x 1024 x 40000 fp32 154 against 177, 2047 x 4096 x 100003 1332 against 1350).  The pieces that become g keep 256 columns: there a
+// narrower tile costs as much in shared memory's traffic as the last round saves.
 Shape logit_shape(int64_t n, int64_t V, int sms)
 {
     Shape s = tile_shape(n, n, V, sms);
-    if (n <= 128 && s.tn == kTileN) {
-        const int64_t rounds = (V + (int64_t)kTileN * sms - 1) / ((int64_t)kTileN * sms);
-        s.tn = (int)up((V + rounds * sms - 1) / (rounds * sms), 32);
+    if (s.tn != kTileN) return s;
+    const int64_t mt = (n + 128 * s.cg - 1) / (128 * s.cg), units = sms / s.cg;
+    int64_t least = INT64_MAX;
+    for (int tn = kTileN; tn >= 128; tn -= 32) {
+        const int64_t rounds = (mt * ((V + tn - 1) / tn) + units - 1) / units, cost = rounds * (tn + 8);        // a tile's fixed cost: some 8 columns
+        if (cost < least) { least = cost; s.tn = tn; }
     }
     return s;
 }
@@ -762,7 +767,7 @@ struct MmaArgs {
     int cols;                // extent of the tile's N axis: classes of the piece, or d (kGrads)
     int kdim;                // extent of the summed axis: d, or classes of the piece (grad_h; grad_w sums over the rows with a target)
     int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
-    int tn;                  // columns of a tile of the logits (kLse, kLogits)
+    int tn;                  // columns of a tile (kLse, kLogits)
     int am;                  // rows in a box of h, and of g for grad_h, where a pair of CTAs does not share the tile
     int v0;                  // first class of the piece
     int k;                   // targets per row (0: one label)
@@ -883,10 +888,10 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
     using S = Smem<CG, KIND, TN>;
     constexpr int NS = S::kStages, SB = S::kStage, BN = TN / CG, kHalf = TN / 2;
     constexpr bool GRADS = KIND == kGrads;
-    // columns of a tile: TN, or fewer where few rows make the time that of reading w (see tile_shape)
+    // columns of a tile: TN, or fewer (see logit_shape)
     // Rows that a tile of 128 has to have loaded: the others' results are not looked at, whatever shared memory holds in their place.
     const int am = CG == 1 ? a.am : 128;
-    const int tn = CG == 1 && TN == kTileN && (KIND == kLse || KIND == kLogits) ? a.tn : TN;
+    const int tn = TN == kTileN && (KIND == kLse || KIND == kLogits) ? a.tn : TN;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     char* const tail = smem_raw + (base - smem_u32(smem_raw)) + NS * SB;
     float* const staging = reinterpret_cast<float*>(tail);
@@ -936,13 +941,13 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
             for (int t = first; t < tiles && ok; t += step) {
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
-                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * tn + (int)rank * BN;
+                const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * tn + (int)rank * (tn / CG);
                 for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
                     const int za = term_a(p), zb = term_b(p);
                     for (int kb = q.k0; kb < q.k1; ++kb) {
                         if (!mbar_wait(empty(s), ph ^ 1u, gave_up)) { ok = false; break; }
                         const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
-                        if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) * 128 - (is_w ? 0 : (128 - am) * 128)));
+                        if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) / CG * 128 - (is_w ? 0 : (128 - am) * 128)));
                         const int x = kb * kTileK;
                         if (is_w) {
                             tma_load<CG>(&mc, dst, bar, ym, x, za);
@@ -1383,8 +1388,9 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         const __nv_bfloat16* wv = wsrc + v0 * wpitch;
         a.v0 = (int)v0;
         if (!w.keep) {
-            a.cols = vn; a.kdim = d; a.am = row_box(w.logits); a.splits = 1;
-            ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, kTileN / w.logits.cg) && launch_mma<kProb, F32>(n, Shape{kTileN, w.logits.cg}, m, a, w, dev, st);
+            const Shape wide = {kTileN, w.logits.cg};
+            a.cols = vn; a.kdim = d; a.am = row_box(wide); a.splits = 1;
+            ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, wide.tn / wide.cg) && launch_mma<kProb, F32>(n, wide, m, a, w, dev, st);
         }
         a.cols = d; a.kdim = vn; a.am = row_box(w.grads); a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
