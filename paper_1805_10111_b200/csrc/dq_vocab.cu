@@ -27,7 +27,6 @@ enum { kLse = 0, kLogits = 1, kProb = 2, kGrads = 3 };
 constexpr int kTileN = 256, kNarrow = 64, kTileK = 64;    // columns of a tile where there are tiles enough for the SMs, and where not
 constexpr int kMaxTop = DQ_VOCAB_MAX_TOP;
 constexpr int kPiece = 16;                                // columns staged at a time where a row has targets among them
-constexpr int kSegment = 8;                               // tiles of K summed in tensor memory before the sum moves to registers
 constexpr int64_t kGradBytes = 256ll << 20;               // bound on the piece of g kept between products
 
 bool ptr_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -869,12 +868,21 @@ __device__ __forceinline__ void store_row(void* out, int64_t at, const float (&f
     }
 }
 
+// Tiles of K that are summed in tensor memory before the sum moves to registers.  The tensor cores cut their fp32 sums off toward zero at
+// every step of 16, which over a long K drifts by about K / 16 * 2^-25 of the sum (measured: 1.0e-5 at K = 4096, 6e-5 at 16384); segments
+// added in registers, rounded to nearest, stop that at 3e-7 (256 of K), 7e-7 (512), 1.3e-6 (1024).  An epilogue takes 2 us to add one, a
+// pair's products 0.26 us a tile of K, so that shorter ones hold the products up (8192 x 4096 x 65536 loss 4.04 ms at 4, 3.14 at 8, 2.85 at
+// 16; 1 x 2048 x 50001 49.9 us at 4, 47.7 at 8).  What is rounded to bf16 next needs none (64: 1e-5 against 2^-9).
+template <int CG, int KIND, bool F32> __host__ __device__ constexpr int segment()
+{
+    if (!F32 && (KIND == kProb || KIND == kGrads)) return 64;
+    return CG == 2 && !F32 ? 16 : 8;
+}
+
 // One persistent kernel per product (kGrads: for the two products that read g).  Warp 0 loads tiles (TMA, 128-byte swizzle), warp 1
 // issues the matrix instructions, warps 4-11 turn finished accumulators into results while the next products run: tensor memory
-// holds two accumulators of 128 rows by 256 columns.  The tensor cores cut their fp32 sums off toward zero at every step, which
-// over a long K drifts by about K / 16 * 2^-25 of the sum (measured: 1.0e-5 at K = 4096, 6e-5 at 16384); so a sum stays in tensor
-// memory for 512 of K and the epilogue adds these segments in registers, rounded to nearest, while the next one runs (7e-7 at any
-// K, for free).  An epilogue thread owns a row's half tile: its maximum and sum need no exchange between threads.
+// holds two accumulators of 128 rows by 256 columns.  An epilogue thread owns a row's half tile: its maximum and sum need no exchange
+// between threads.
 // CG = 2: two CTAs on neighbouring SMs share a tile of 256 rows.  Each loads its 128 rows and half of the columns' operand; the
 // even one issues for both.
 // Operands: logits h (A) and w (B), both along d.  grad_h: g along the classes, w across.  grad_w: g and h, both across; its K axis
@@ -888,6 +896,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
     using S = Smem<CG, KIND, TN>;
     constexpr int NS = S::kStages, SB = S::kStage, BN = TN / CG, kHalf = TN / 2;
     constexpr bool GRADS = KIND == kGrads;
+    constexpr int kSegment = segment<CG, KIND, F32>();
     // columns of a tile: TN, or fewer (see logit_shape)
     // Rows that a tile of 128 has to have loaded: the others' results are not looked at, whatever shared memory holds in their place.
     const int am = CG == 1 ? a.am : 128;
@@ -1074,13 +1083,15 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                     for (int c = 0; c < kHalf; c += 32) tmem_ld32(d + c, reinterpret_cast<uint32_t (&)[32]>(f[c]));
                     tmem_wait_ld();
                 } else {
+                    // the next 32 columns are on their way while these are added
+                    uint32_t v[2][32];
+                    tmem_ld32(d, v[0]);
 #pragma unroll
                     for (int c = 0; c < kHalf; c += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(d + c, v);
                         tmem_wait_ld();
+                        if (c + 32 < kHalf) tmem_ld32(d + c + 32, v[c / 32 + 1 & 1]);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) f[c + j] += __uint_as_float(v[j]);
+                        for (int j = 0; j < 32; ++j) f[c + j] += __uint_as_float(v[c / 32 & 1][j]);
                     }
                 }
                 fence_before_sync();
