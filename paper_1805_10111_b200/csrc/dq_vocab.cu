@@ -1,14 +1,15 @@
 // Losses of a large output layer (a vocabulary of V classes) and their gradients: softmax cross-entropy and distillation
-// from a teacher's top logits.  z = h w^T is formed in tiles of tensor memory and never kept.
+// from a teacher's top logits.  The logits z = h w^T are formed in tiles of tensor memory; at most 256 MB of them are ever kept.
 //
 // Mathematics.  With c = 1/T (T = 1 for cross-entropy), lse_n = log sum_v exp(c z_nv) and a row's targets (i_k, q_k),
 // S = sum q_k (cross-entropy: one target, q = 1):
 //   loss_n = T^2 sum_k q_k (log q_k - (c z_n,ik - lse_n)),    dF/dz_nv = weight_n T (S_n p_nv - sum_{k: i_k = v} q_k) =: g_nv,
 //   grad_h = g w,   grad_w = g^T h.
 // Plan.  Rows without a target are left out at the start: the others are gathered into a compact copy of h (so padding costs
-// nothing and a NaN in a padded row reaches nothing).  One pass of products leaves (max, sum) per row and 256 columns; a small
-// kernel joins them to lse and the loss.  For the gradient the logits are formed again, a piece of the vocabulary at a time,
-// turned into g (rounded to bf16) in the kernel's epilogue, and two more products read the piece while it is warm.
+// nothing and a NaN in a padded row reaches nothing).  One pass of products leaves (max, sum) per row and half tile; a small
+// kernel joins them to lse and the loss.  For the gradient the logits are read back where they were few enough to be kept, else formed
+// again a piece of the vocabulary at a time, and turned into g (rounded to bf16; three terms for fp32); two more products, in one
+// launch, read the piece while it is warm.  Up to eight fp32 rows go through kernels of their own (vocab_few_*).
 // Every sum has a fixed order: equal inputs give equal bytes.
 #include <math.h>
 #include <atomic>
@@ -72,17 +73,19 @@ struct Work {
     __nv_bfloat16* wp;             // [terms][V][dp] w, where it cannot be read in place
     float* z;                      // [n_pad][vc] the logits, where they are few enough to be kept (see run_loss)
     float2* part;                  // [n_pad][parts] (max, sum) of a row's half tiles, see join_pair
-    __nv_bfloat16* g;              // [terms][n_pad][vc] piece of the logits' gradient
+    __nv_bfloat16* g;              // [gterms][n_pad][vc] piece of the logits' gradient
     float* gf;                     // few rows: the logits' gradient [V][few]
     float* dh;                     // [splits][n_pad][dq] sums of grad_h
     // sizes
-    int terms; int64_t n_pad, dp, dq, vc; int parts, splits, kps; bool direct_w, keep;
+    int terms, gterms;             // bf16 terms of h and w, of g
+    int64_t n_pad, dp, dq, vc; int parts, splits, kps; bool direct_w, keep;
     int few;                       // rows that the products of few rows work on, 2 or 8; 0: tensor cores
     int chunks; int64_t span;      // their gradients' blocks: pieces of 128 columns, classes of a block
     Shape logits, grads;           // tiles of the products
     int64_t bytes;
 };
 
+constexpr int kTwoTerms = 16;                             // rows up to which g of bf16 calls has two terms
 constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
 __host__ __device__ constexpr int few_blocks(int rows) { return rows == 2 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
 
@@ -133,13 +136,18 @@ Work carve(const dq_vocab* v, bool grad, int sms)
     if (!w.direct_w) w.wp = (__nv_bfloat16*)take(2 * w.terms * v->V * w.dp);
     w.part = (float2*)take(8 * w.n_pad * w.parts);
     if (grad) {
-        int64_t vc = kGradBytes / (2 * w.terms * w.n_pad) / kTileN * kTileN;
+        // g is rounded to bf16, as its values are many and their errors independent; with few rows they are not (one row: grad_w is one
+        // rounded number times h), and a second term costs little (8 x 256 x 1000: 23 us against 20, errors against 64 bits 0.0016 instead of up
+        // to 0.0026; 64 x 2048 x 65536 would take 230 us against 207 for 0.0017 instead of 0.0020).
+        w.gterms = f32 ? 3 : v->n <= 128 ? 2 : 1;
+        int64_t vc = kGradBytes / (2 * w.gterms * w.n_pad) / kTileN * kTileN;
         if (vc < 2 * kTileN) vc = 2 * kTileN;
         if (vc > up(v->V, kTileN)) vc = up(v->V, kTileN);
         const int64_t pieces = (v->V + vc - 1) / vc;                       // pieces of nearly the same size
         w.vc = up((v->V + pieces - 1) / pieces, kTileN);
-        w.g = (__nv_bfloat16*)take(2 * w.terms * w.n_pad * w.vc);
         w.keep = w.vc >= v->V && 4 * w.n_pad * w.vc <= kGradBytes;
+        if (w.keep && !f32 && v->n > kTwoTerms) w.gterms = 1;
+        w.g = (__nv_bfloat16*)take(2 * w.gterms * w.n_pad * w.vc);
         if (w.keep) w.z = (float*)take(4 * w.n_pad * w.vc);
         // few rows: grad_h has fewer tiles than the GPU has SMs, so its sum over the vocabulary is split and joined
         w.grads = tile_shape(v->n, w.vc > v->n ? w.vc : v->n, v->d, sms);
@@ -380,20 +388,21 @@ __device__ __forceinline__ void warp_join(float& m, float& s, float c2)         
     for (int o = 16; o > 0; o >>= 1) join_pair(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o), c2);
 }
 
-// A row's loss, by a warp: zt(j) is the logit at its target j.  lse is formed in double and rounded once; the loss is what fp32 gives for
+// A row's loss, by a warp: zt(j) is the logit at its target j, `drift` the part of the logits that is to be added to them (c2 holds it already,
+// see logit_drift).  lse is formed in double and rounded once; the loss is what fp32 gives for
 // lse - z / T, so that it is the loss of the lse that the caller gets (half a step of lse off at most).
 template <class Z>
-__device__ __forceinline__ void write_loss(const Work& w, int64_t row, int k, float2 ms, float temp, float* loss, float* lse, Z zt)
+__device__ __forceinline__ void write_loss(const Work& w, int64_t row, int k, float2 ms, float temp, float drift, float* loss, float* lse, Z zt)
 {
-    const float l = (float)((double)ms.x / (double)temp + log((double)ms.y));
+    const float l = (float)((double)__fmaf_rn(ms.x, drift, ms.x) / (double)temp + log((double)ms.y));
     const int lane = threadIdx.x & 31;
     if (k == 0) {
-        if (lane == 0) loss[row] = l - zt(0);
+        if (lane == 0) loss[row] = __fsub_rn(l, __fmaf_rn(zt(0), drift, zt(0)));
     } else {
         double sum = 0.0;
         for (int j = lane; j < k; j += 32) {
             const float q = w.eq[row * k + j];
-            if (w.eidx[row * k + j] != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - (double)(__fdiv_rn(zt(j), temp) - l));
+            if (w.eidx[row * k + j] != INT32_MAX && q != 0.0f) sum += (double)q * ((double)w.elq[row * k + j] - (double)__fsub_rn(__fdiv_rn(__fmaf_rn(zt(j), drift, zt(j)), temp), l));
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -403,7 +412,7 @@ __device__ __forceinline__ void write_loss(const Work& w, int64_t row, int k, fl
 }
 
 // Joins a row's pairs, forms the loss and the two factors of the gradient; a warp per row.
-__global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+__global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const float* __restrict__ weight, float temp, float c2, float drift, float* __restrict__ loss,
                                                          float* __restrict__ lse)
 {
     pdl_prologue();
@@ -414,7 +423,7 @@ __global__ void __launch_bounds__(256) vocab_join_kernel(Work w, int k, const fl
         for (int t = lane; t < w.parts; t += 32) join_pair(m, s, p[t].x, p[t].y, c2);
         warp_join(m, s, c2);
         const int64_t row = w.map[i];
-        write_loss(w, row, k, make_float2(m, s), temp, loss, lse, [&](int j) { return w.zt[row * (k > 0 ? k : 1) + j]; });
+        write_loss(w, row, k, make_float2(m, s), temp, drift, loss, lse, [&](int j) { return w.zt[row * (k > 0 ? k : 1) + j]; });
         // The mean's factor T / count is left to the end: p - q is rounded to bf16 next, and for the entry that matters most,
         // p - 1 just inside (-1, 0), the rounding is smallest without it (2^-9 at most, 2^-8 with an unlucky factor)
         const float wt = weight ? weight[row] * temp : 1.0f;
@@ -441,13 +450,12 @@ __device__ __forceinline__ float2 block_join(const float2* p, int parts, float c
 // from L2 against a launch).  Part 0 also writes the loss.  Rows behind the last one, up to a whole tile of K, and columns behind the
 // vocabulary are zeros: the gradients' products read them.
 constexpr int kRowCols = 2048;
-template <bool F32>
+template <int TERMS>
 __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, int parts_per_row, const int32_t* __restrict__ labels,
-                                                         const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+                                                         const float* __restrict__ weight, float temp, float c2, float drift, float* __restrict__ loss,
                                                          float* __restrict__ lse)
 {
     pdl_prologue();
-    constexpr int TERMS = F32 ? 3 : 1;
     const int count = w.ctrl->count, i = blockIdx.x / parts_per_row, part = blockIdx.x % parts_per_row;
     if (i >= (count + kTileK - 1) / kTileK * kTileK) return;
     const int64_t plane = w.n_pad * w.vc;
@@ -468,7 +476,7 @@ __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, i
     const float2 ms = block_join(w.part + (int64_t)i * w.parts, w.parts, c2);
     const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
     if (part == 0 && threadIdx.x < 32)
-        write_loss(w, row, k, ms, temp, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
+        write_loss(w, row, k, ms, temp, drift, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
     while (col < hi) {
         float e[8];
 #pragma unroll
@@ -672,7 +680,7 @@ __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, floa
 // lse and loss, and g [classes][NR] as fp32 where it is wanted; a block takes part of a row's columns.
 template <int NR>
 __global__ void __launch_bounds__(256) vocab_few_rows_kernel(Work w, int n, int V, int k, int parts_per_row, bool grad, const int32_t* __restrict__ labels,
-                                                             const float* __restrict__ weight, float temp, float c2, float* __restrict__ loss,
+                                                             const float* __restrict__ weight, float temp, float c2, float drift, float* __restrict__ loss,
                                                              float* __restrict__ lse)
 {
     pdl_prologue();
@@ -686,7 +694,7 @@ __global__ void __launch_bounds__(256) vocab_few_rows_kernel(Work w, int n, int 
     const float2 ms = block_join(w.part + (int64_t)row * w.parts, w.parts, c2);
     const float mass = k > 0 ? w.emass[row] : 1.0f, wt = weight ? weight[row] * temp : 1.0f, scale = wt * mass / ms.y;
     if (part == 0 && threadIdx.x < 32)
-        write_loss(w, row, k, ms, temp, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
+        write_loss(w, row, k, ms, temp, drift, loss, lse, [&](int j) { return z[k > 0 ? w.eidx[(int64_t)row * k + j] : labels[row]]; });
     if (!grad) return;
 #pragma unroll 4
     for (int col = lo + threadIdx.x; col < hi; col += 256) w.gf[(int64_t)col * NR + row] = scale * ex2((z[col] - ms.x) * c2);
@@ -765,7 +773,7 @@ __global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(co
 struct MmaArgs {
     int cols;                // extent of the tile's N axis: classes of the piece, or d (kGrads)
     int kdim;                // extent of the summed axis: d, or classes of the piece (grad_h; grad_w sums over the rows with a target)
-    int pairs;               // products of bf16 terms: 1, or 6 for fp32 operands
+    int pairs;               // products of bf16 terms: 6 for fp32 operands, 2 for two terms of g, else 1
     int tn;                  // columns of a tile (kLse, kLogits)
     int am;                  // rows in a box of h, and of g for grad_h, where a pair of CTAs does not share the tile
     int v0;                  // first class of the piece
@@ -780,10 +788,10 @@ struct MmaArgs {
     int align_h, align_w;    // rows of the output start on 16 bytes (1), 32 (2) or neither (0)
 };
 
-// Products of bf16 terms for fp32 operands, smallest first so that the leading one is rounded least: (2,0) (0,2) (1,1) (1,0)
-// (0,1) (0,0).  What is left out is below 2^-26 of |a||b|.
-__device__ __forceinline__ int term_a(int p) { return (0x001102 >> (4 * p)) & 15; }
-__device__ __forceinline__ int term_b(int p) { return (0x010120 >> (4 * p)) & 15; }
+// Products of bf16 terms for fp32 operands, smallest first so that the leading one is rounded least: (2,0) (0,2) (1,1) (0,1)
+// (1,0) (0,0).  What is left out is below 2^-26 of |a||b|.  Two terms of g with bf16 operands: the last two.
+__device__ __forceinline__ int term_a(int p) { return (0x010102 >> (4 * p)) & 15; }
+__device__ __forceinline__ int term_b(int p) { return (0x001120 >> (4 * p)) & 15; }
 
 // Shared memory of a product: NS stages of both operands' tiles, and for each epilogue warp either one piece of columns (targets
 // are looked up in it) or two buffers of 32 rows by 128 bytes on their way out by TMA.
@@ -879,6 +887,17 @@ template <int CG, int KIND, bool F32> __host__ __device__ constexpr int segment(
     return CG == 2 && !F32 ? 16 : 8;
 }
 
+// What the cut-off takes from a sum on average, given back to the logits with the factor 1 / T.  A step cuts off half a unit in the last
+// place: 2^-25 log2(e) of the running sum for significands spread evenly in the logarithm.  Whatever order the terms come in, the sum at step i
+// of n has i / n of its end value on average, so that a segment of n steps loses n 2^-26 log2(e) of itself.  Measured at n = 32: 0.84 of that
+// for terms of one sign, 0.58 for random ones, 1.0 for random ones with a common part.  Three quarters are given back, which leaves 1e-7 to
+// 2e-7 of the 4e-7 to 7e-7 that were off.
+inline float logit_drift(int d, int segment_tiles)
+{
+    const int steps = (d + 15) / 16, most = segment_tiles * (kTileK / 16);
+    return (float)((steps < most ? steps : most) * (0.75 * 1.4426950408889634 / 67108864.0));
+}
+
 // One persistent kernel per product (kGrads: for the two products that read g).  Warp 0 loads tiles (TMA, 128-byte swizzle), warp 1
 // issues the matrix instructions, warps 4-11 turn finished accumulators into results while the next products run: tensor memory
 // holds two accumulators of 128 rows by 256 columns.  An epilogue thread owns a row's half tile: its maximum and sum need no exchange
@@ -951,9 +970,13 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
                 const Tile q = tile(t);
                 const bool is_w = GRADS && t >= tiles_h;
                 const int ym = q.m * 128 * CG + (int)rank * 128, yn = q.n * tn + (int)rank * (tn / CG);
-                for (int p = 6 - a.pairs; p < 6 && ok; ++p) {
-                    const int za = term_a(p), zb = term_b(p);
-                    for (int kb = q.k0; kb < q.k1; ++kb) {
+                // terms outside, K inside; two terms of g the other way round, so that the second finds the other operand in L2
+                const bool inner = GRADS && !F32 && a.pairs == 2;
+                const int outs = inner ? 1 : a.pairs, ins = inner ? 2 : 1;
+                for (int po = 6 - outs; po < 6 && ok; ++po) {
+                    for (int i = q.k0 * ins; i < q.k1 * ins; ++i) {
+                        const int p = inner ? 4 + (i & 1) : po, kb = inner ? i >> 1 : i;
+                        const int za = term_a(p), zb = term_b(p);
                         if (!mbar_wait(empty(s), ph ^ 1u, gave_up)) { ok = false; break; }
                         const uint32_t dst = base + s * SB, bar = CG == 2 ? map_to_cta(full(s), 0) : full(s);
                         if (rank == 0) mbar_expect_tx(full(s), CG * (SB - (TN - tn) / CG * 128 - (is_w ? 0 : (128 - am) * 128)));
@@ -1156,7 +1179,7 @@ __global__ void __launch_bounds__(384, 1) vocab_mma_kernel(const __grid_constant
 #pragma unroll
                         for (int j = 0; j < kPiece; ++j) f[c + j] = stage[j * 32];
                     }
-                    store_terms<F32 ? 3 : 1>(o + c, w.n_pad * w.vc, f + c, true);
+                    store_terms<F32 ? 3 : CG == 1 ? 2 : 1>(o + c, w.n_pad * w.vc, f + c, true);
                 }
             } else {
                 bool out = r < (is_w ? a.kdim : count);
@@ -1329,7 +1352,7 @@ int run_few(const dq_vocab* v, const Targets& t, float* loss, float* lse, const 
     ok = ok && launch_k(vocab_few_logits_kernel<NR>, dim3((unsigned)w.parts), dim3(256), 0, st, q, c2, loss, lse, w) == cudaSuccess;
     const int parts_per_row = g ? (int)min((int64_t)32, (v->V + 1023) / 1024) : 1;
     ok = ok && launch_k(vocab_few_rows_kernel<NR>, dim3((unsigned)((g ? NR : n) * parts_per_row)), dim3(256), 0, st, w, n, V, k, parts_per_row, g != nullptr, t.labels,
-                        g ? g->weight : (const float*)nullptr, t.temp, c2, loss, lse) == cudaSuccess;
+                        g ? g->weight : (const float*)nullptr, t.temp, c2, 0.0f, loss, lse) == cudaSuccess;
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
     const float scale = g->weight ? 0.0f : t.temp;
     ok = ok && launch_k(vocab_few_grads_kernel<NR>, dim3((unsigned)(w.chunks * w.splits)), dim3(256), 0, st, q, scale, static_cast<float*>(g->gw), g->ld_w,
@@ -1364,8 +1387,9 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     const int64_t wpitch = w.direct_w ? v->ld_w : w.dp;
 
     // logits: boxes along d, of 128 rows of h and a CTA's share of a tile's rows of w
+    const float drift = logit_drift(d, w.logits.cg == 2 ? segment<2, kLse, F32>() : segment<1, kLse, F32>());
     MmaArgs a = {};
-    a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
+    a.pairs = F32 ? 6 : 1; a.k = k; a.c2 = (float)(1.4426950408889634 * (1.0 + drift) / (double)t.temp); a.eidx = k > 0 ? w.eidx : t.labels;
     a.splits = 1; a.scale = g && !g->weight ? t.temp : 0.0f;
     Maps m = {};
     auto row_box = [&](const Shape& x) { return x.cg == 2 || n > 120 ? 128 : (int)up(n, 8); };
@@ -1380,17 +1404,18 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         ok = ok && launch_mma<kLogits, F32>(n, w.logits, m, a, w, dev, st);
         const int64_t rows = up(n, kTileK);
         const int per_row = (int)min((w.vc + kRowCols - 1) / kRowCols, (4 * dev.sms + n - 1) / n);      // some blocks for every SM
-        ok = ok && launch_k(vocab_rows_kernel<F32>, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, w, (int)V, k, per_row, t.labels, weight, t.temp, a.c2,
+        auto rows_kernel = F32 ? vocab_rows_kernel<3> : w.gterms == 2 ? vocab_rows_kernel<2> : vocab_rows_kernel<1>;
+        ok = ok && launch_k(rows_kernel, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, w, (int)V, k, per_row, t.labels, weight, t.temp, a.c2, drift,
                             loss, lse) == cudaSuccess;
     } else {
         ok = ok && launch_mma<kLse, F32>(n, w.logits, m, a, w, dev, st);
-        ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, weight, t.temp, a.c2, loss, lse) == cudaSuccess;
+        ok = ok && launch_k(vocab_join_kernel, dim3((unsigned)min((int64_t)blocks, (n + 7) / 8)), dim3(256), 0, st, w, k, weight, t.temp, a.c2, drift, loss, lse) == cudaSuccess;
     }
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
 
     // gradients, a piece of the vocabulary at a time
     Maps u = {};
-    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, row_box(w.grads)) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, T, w.n_pad * w.vc, kTileK) &&
+    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, w.gterms, w.n_pad * w.vc, row_box(w.grads)) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, w.gterms, w.n_pad * w.vc, kTileK) &&
          make_map(&u.m[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
     a.gh = g->gh; a.gw = g->gw; a.ld_gh = g->ld_h; a.ld_gw = g->ld_w; a.kps = w.kps;
     a.align_h = row_alignment(g->gh, g->ld_h * elem); a.align_w = row_alignment(g->gw, g->ld_w * elem);
@@ -1400,9 +1425,11 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         a.v0 = (int)v0;
         if (!w.keep) {
             const Shape wide = {kTileN, w.logits.cg};
+            a.pairs = F32 ? 6 : 1;
             a.cols = vn; a.kdim = d; a.am = row_box(wide); a.splits = 1;
             ok = make_map(&m.m[1], wv, d, vn, wpitch, T, V * wpitch, wide.tn / wide.cg) && launch_mma<kProb, F32>(n, wide, m, a, w, dev, st);
         }
+        a.pairs = F32 ? 6 : w.gterms;
         a.cols = d; a.kdim = vn; a.am = row_box(w.grads); a.first = v0 == 0; a.last = v0 + w.vc >= V;
         a.splits = (int)(((vn + kTileK - 1) / kTileK + w.kps - 1) / w.kps);
         u.m[4] = u.m[3];                                   // (a valid map, though one for grad_w is not used without alignment)
