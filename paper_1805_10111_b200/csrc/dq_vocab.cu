@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(256) vocab_targets_kernel(const int32_t* __res
 
 // Compact copy of the rows that have a target.  A block owns a range of rows; it counts the targets before its range (the list
 // is small and in L2) instead of waiting for a scan, then copies its own rows warp by warp.  Rows without a target get loss 0,
-// lse 0 and their zero row of grad_h here.  The last block writes the count and zeroes h's rows up to a whole tile of K (a zero of g times whatever the
-// buffer held would be NaN).
+// lse 0 and their zero row of grad_h here.  The last block writes the count and zeroes h's rows up to a whole tile of K (a zero of g times
+// whatever the buffer held would be NaN); the tensor maps end at row n.
 template <bool F32>
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restrict__ h, int64_t ld, int d, const int32_t* __restrict__ tgt, int64_t V,
                                                            int64_t n, int64_t rows_per_block, bool vec, float* loss, float* lse, void* gh,
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
     }
     if (blockIdx.x == q.first - 1) {
         if (threadIdx.x == 0) { w.ctrl->count = before; w.ctrl->status = DQ_OK; }
-        const int end = (before + kTileK - 1) / kTileK * kTileK;
+        const int end = (int)min(n, ((int64_t)before + kTileK - 1) / kTileK * kTileK);
         for (int i = before + warp; i < end; i += 8)
             for (int t = 0; t < w.terms; ++t)
                 for (int j = lane * 8; j < w.dp; j += 256)
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(256) vocab_rows_kernel(Work w, int V, int k, i
 {
     pdl_prologue();
     const int count = w.ctrl->count, i = blockIdx.x / parts_per_row, part = blockIdx.x % parts_per_row;
-    if (i >= (count + kTileK - 1) / kTileK * kTileK) return;
+    if (i >= (count + kTileK - 1) / kTileK * kTileK) return;               // (rows from n on read as zeros anyway: the maps end there)
     const int64_t plane = w.n_pad * w.vc;
     const int vc = (int)w.vc, span = (vc / parts_per_row + kRowCols) / kRowCols * kRowCols, lo = part * span, hi = min(vc, lo + span);
     if (lo >= hi) return;
@@ -1393,7 +1393,7 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
     a.splits = 1; a.scale = g && !g->weight ? t.temp : 0.0f;
     Maps m = {};
     auto row_box = [&](const Shape& x) { return x.cg == 2 || n > 120 ? 128 : (int)up(n, 8); };
-    ok = ok && make_map(&m.m[0], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, row_box(w.logits)) &&
+    ok = ok && make_map(&m.m[0], w.hp, d, n, w.dp, T, w.n_pad * w.dp, row_box(w.logits)) &&
          make_map(&m.m[1], wsrc, d, V, wpitch, T, V * wpitch, w.logits.tn / w.logits.cg);
     if (w.keep) ok = ok && make_out_map(&m.m[4], true, w.z, w.vc, w.n_pad, w.vc);
     a.cols = (int)V; a.kdim = d; a.tn = w.logits.tn; a.am = row_box(w.logits);
@@ -1402,10 +1402,9 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
         // The logits of the whole vocabulary fit where a piece of g may be: form them once.  Writing and reading them (8 bytes each) is
         // cheaper than forming them again (2 d flops, six times that for fp32) and merges the join with what follows it.
         ok = ok && launch_mma<kLogits, F32>(n, w.logits, m, a, w, dev, st);
-        const int64_t rows = up(n, kTileK);
         const int per_row = (int)min((w.vc + kRowCols - 1) / kRowCols, (4 * dev.sms + n - 1) / n);      // some blocks for every SM
         auto rows_kernel = F32 ? vocab_rows_kernel<3> : w.gterms == 2 ? vocab_rows_kernel<2> : vocab_rows_kernel<1>;
-        ok = ok && launch_k(rows_kernel, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, w, (int)V, k, per_row, t.labels, weight, t.temp, a.c2, drift,
+        ok = ok && launch_k(rows_kernel, dim3((unsigned)(n * per_row)), dim3(256), 0, st, w, (int)V, k, per_row, t.labels, weight, t.temp, a.c2, drift,
                             loss, lse) == cudaSuccess;
     } else {
         ok = ok && launch_mma<kLse, F32>(n, w.logits, m, a, w, dev, st);
@@ -1415,8 +1414,9 @@ int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const
 
     // gradients, a piece of the vocabulary at a time
     Maps u = {};
-    ok = ok && make_map(&u.m[0], w.g, w.vc, w.n_pad, w.vc, w.gterms, w.n_pad * w.vc, row_box(w.grads)) && make_map(&u.m[2], w.g, w.vc, w.n_pad, w.vc, w.gterms, w.n_pad * w.vc, kTileK) &&
-         make_map(&u.m[3], w.hp, d, w.n_pad, w.dp, T, w.n_pad * w.dp, kTileK);
+    ok = ok && make_map(&u.m[0], w.g, w.vc, n, w.vc, w.gterms, w.n_pad * w.vc, row_box(w.grads)) &&
+         make_map(&u.m[2], w.g, w.vc, n, w.vc, w.gterms, w.n_pad * w.vc, kTileK) &&
+         make_map(&u.m[3], w.hp, d, n, w.dp, T, w.n_pad * w.dp, kTileK);
     a.gh = g->gh; a.gw = g->gw; a.ld_gh = g->ld_h; a.ld_gw = g->ld_w; a.kps = w.kps;
     a.align_h = row_alignment(g->gh, g->ld_h * elem); a.align_w = row_alignment(g->gw, g->ld_w * elem);
     for (int64_t v0 = 0; v0 < V && ok; v0 += w.vc) {
@@ -1500,8 +1500,8 @@ int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
         const int64_t bytes = carve(&u, grad != 0, dev.sms).bytes;
         if (bytes > most) most = bytes;
     };
-    for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128, but for few rows
-    see(v->n); see(2); see(kFewRows);
+    for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128, but for a few rows
+    see(v->n); see(2); see(kFewRows); see(kTwoTerms);
     return most;
 }
 

@@ -371,7 +371,7 @@ def test_graph_replay_streams_and_reused_workspace(dq):
         ref2.check(*out2, where="second stream")
     need = dq.Vocab.workspace_bytes(h, w)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-    for n in (400, 1, 130, 400):                                             # fewer rows fit into the same workspace
+    for n in (400, 1, 16, 17, 130, 400):                                     # fewer rows fit into the same workspace
         small = dq.Vocab(h[:n], w, workspace=ws)
         o = _outputs(h[:n], w)
         assert dq.dq_xent_grad(small, labels[:n], None, *o) == 0
@@ -526,3 +526,18 @@ print("captured")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+def test_workspace_is_enough_for_fewer_rows(dq):
+    """dq_vocab_workspace_bytes covers every number of rows up to n, whatever form a call of that many takes."""
+    torch = _torch()
+    for dt in (torch.bfloat16, torch.float32):
+        for d, V in ((64, 1000), (1536, 9791), (24, 70001)):
+            w = torch.zeros(V, d, dtype=dt, device="cuda")
+            for grad in (False, True):
+                for n in (1, 2, 8, 9, 16, 17, 100, 128, 129, 256, 257, 700):
+                    h = torch.zeros(n, d, dtype=dt, device="cuda")
+                    most = dq.Vocab.workspace_bytes(h, w, grad=grad)
+                    for m in (1, 2, 3, 8, 9, 16, 17, 64, 128, 129, 250, 256, 384, 385, 512, 640):
+                        if m <= n:
+                            assert dq.Vocab.workspace_bytes(h[:m], w, grad=grad) <= most, (dt, d, V, grad, n, m)
