@@ -541,3 +541,36 @@ def test_workspace_is_enough_for_fewer_rows(dq):
                     for m in (1, 2, 3, 8, 9, 16, 17, 64, 128, 129, 250, 256, 384, 385, 512, 640):
                         if m <= n:
                             assert dq.Vocab.workspace_bytes(h[:m], w, grad=grad) <= most, (dt, d, V, grad, n, m)
+
+
+@pytest.mark.parametrize("dt,n,d,V", [("bfloat16", 100, 24, 300_001), ("float32", 20, 16, 300_001), ("bfloat16", 4, 65536, 70),
+                                      ("float32", 40, 40_000, 130), ("float32", 3, 65535, 40), ("bfloat16", 20_000, 8, 9),
+                                      ("float32", 20_001, 5, 3), ("bfloat16", 700, 3, 70_000)])
+def test_ends_of_the_ranges(dq, dt, n, d, V):
+    """Few rows over more classes than the kept logits may be, the widest rows, many rows of almost nothing."""
+    torch = _torch()
+    g, h, w, labels = _inputs(n, d, V, getattr(torch, dt), 50, scale=1.0)
+    labels[0] = V - 1
+    if n > 50:
+        labels[3::7] = -1
+    xent_ref(h, w, labels).check(*xent(dq, h, w, labels))
+    idx, t = _entries(g, n, V, 3, labels.clamp(min=0))
+    distill_ref(h, w, idx, t, None, 2.0).check(*distill(dq, h, w, idx, t, None, 2.0))
+
+
+def test_two_streams_at_once(dq):
+    """Calls of two holders overlap on two streams, many times over; every result equals that of the call alone, byte for byte."""
+    torch = _torch()
+    jobs = []
+    for seed, (dt, n, d, V) in enumerate((("bfloat16", 600, 256, 9000), ("float32", 300, 128, 5000))):
+        _, h, w, labels = _inputs(n, d, V, getattr(torch, dt), 60 + seed)
+        jobs.append((dq.Vocab(h, w), labels, _outputs(h, w), xent(dq, h, w, labels), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for layer, labels, out, _, stream in jobs:
+            with torch.cuda.stream(stream):
+                assert dq.dq_xent_grad(layer, labels, None, *out) == 0
+    torch.cuda.synchronize()
+    for layer, _, out, alone, _ in jobs:
+        assert all(torch.equal(a, b) for a, b in zip(out, alone))
+        assert dq.dq_vocab_status(layer) == (0, 0)
