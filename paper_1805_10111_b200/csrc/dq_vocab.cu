@@ -79,7 +79,7 @@ struct Work {
     // sizes
     int terms, gterms;             // bf16 terms of h and w, of g
     int64_t n_pad, dp, dq, vc; int parts, splits, kps; bool direct_w, keep;
-    int few;                       // rows that the products of few rows work on, 2 or 8; 0: tensor cores
+    int few;                       // rows that the products of few rows work on, 2, 4 or 8; 0: tensor cores
     int chunks; int64_t span;      // their gradients' blocks: pieces of 128 columns, classes of a block
     Shape logits, grads;           // tiles of the products
     int64_t bytes;
@@ -87,7 +87,7 @@ struct Work {
 
 constexpr int kTwoTerms = 16;                             // rows up to which g of bf16 calls has two terms
 constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
-__host__ __device__ constexpr int few_blocks(int rows) { return rows == 2 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
+__host__ __device__ constexpr int few_blocks(int rows) { return rows < 8 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
 
 Work carve(const dq_vocab* v, bool grad, int sms)
 {
@@ -113,7 +113,7 @@ Work carve(const dq_vocab* v, bool grad, int sms)
         w.eidx = (int32_t*)take(4 * w.n_pad * k); w.eq = (float*)take(4 * w.n_pad * k); w.elq = (float*)take(4 * w.n_pad * k);
     }
     if (few) {
-        w.few = v->n <= 2 ? 2 : 8;
+        w.few = v->n <= 2 ? 2 : v->n <= 4 ? 4 : 8;
         const int64_t groups = (v->V + (w.few == 8 ? 31 : 63)) / (w.few == 8 ? 32 : 64);       // classes that a block takes at a time
         w.parts = (int)(groups < 2 * sms ? groups : 2 * sms);
         w.vc = up(v->V, 8);
@@ -554,11 +554,11 @@ __global__ void __launch_bounds__(256) vocab_grad_h_kernel(Work w, int n, int d,
 // ---- few rows of fp32: products on the CUDA cores ------------------------------------------------------------------------------
 
 // Up to eight rows of fp32: such calls are bound by reading w, which these kernels read as it is; the tensor cores would need its
-// bf16 terms first (10 more bytes a value) and take six products of them (1 x 2048 x 50001: loss 75 us against 393, gradient 243
-// against 726; 8 x 64 x 100: 8 and 16 us against 15 and 23).  bf16 weights feed the tensor cores without a copy, which is faster at any
+// bf16 terms first (10 more bytes a value) and take six products of them (1 x 2048 x 50001: loss 68 us against 390, gradient 216
+// against 715; 8 x 4096 x 30000 gradient 429 against 827; 8 x 64 x 100: 8 and 16 us against 15 and 22).  bf16 weights feed the tensor cores without a copy, which is faster at any
 // size (1 x 2048 x 50001: 54 us).  Everything is fp32, g too.  No compact copy of the rows: one without a target counts as zeros.
 
-struct Few { const float *h, *w; int64_t ld_h, ld_w; int n, d; int64_t V; const int32_t* tgt; bool vec_h, vec_w; };
+struct Few { const float *h, *w; int64_t ld_h, ld_w; int n, d; int64_t V; const int32_t* tgt; };
 
 // Which rows have a target, one bit each.
 __device__ __forceinline__ uint32_t few_mask(const Few& q)
@@ -568,11 +568,12 @@ __device__ __forceinline__ uint32_t few_mask(const Few& q)
     return __ballot_sync(0xFFFFFFFFu, t >= 0 && t < q.V);
 }
 
-// Values k .. k + 3 of a row; zeros from `d` on.  The weights pass the L1 by.
-__device__ __forceinline__ float4 few_load(const float* p, int k, int d, bool vec)
+// Values k .. k + 3 of a row; zeros from `d` on.  The weights pass the L1 by.  VEC: rows start on 16 bytes and d is a multiple of 4.
+template <bool VEC>
+__device__ __forceinline__ float4 few_load(const float* p, int k, int d)
 {
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (vec && k + 4 <= d) {
+    if (VEC) {
         asm("ld.global.nc.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p + k));
     } else {
         if (k < d) x.x = __ldg(p + k);
@@ -609,7 +610,7 @@ __device__ __forceinline__ void warp_transpose_sum(float (&v)[N], int lane)
 
 // Logits of NR rows, CW classes to a warp, K over the lanes in 16-byte loads, h in shared memory 1024 columns at a time; (max, sum) per
 // row and block.  Block 0 opens the call: the status, the number of rows with a target, the others' zero results.
-template <int NR>
+template <int NR, bool VEC>
 __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, float c2, float* __restrict__ loss, float* __restrict__ lse, Work w)
 {
     pdl_prologue();
@@ -636,7 +637,7 @@ __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, floa
 #pragma unroll
                 for (int i = 0; i < NR; ++i) {
                     const int k = k0 + threadIdx.x * 4;
-                    s_h[i][threadIdx.x] = mask >> i & 1 ? few_load(q.h + i * q.ld_h, k, q.d, q.vec_h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    s_h[i][threadIdx.x] = mask >> i & 1 && k < q.d ? few_load<VEC>(q.h + i * q.ld_h, k, q.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 }
                 held = k0;
                 __syncthreads();
@@ -646,7 +647,7 @@ __global__ void __launch_bounds__(256) vocab_few_logits_kernel(const Few q, floa
             for (int k = lane * 4; k < kn; k += 128) {
                 float4 y[CW];
 #pragma unroll
-                for (int j = 0; j < CW; ++j) y[j] = few_load(q.w + min(v + j, q.V - 1) * q.ld_w, k0 + k, q.d, q.vec_w);
+                for (int j = 0; j < CW; ++j) y[j] = few_load<VEC>(q.w + min(v + j, q.V - 1) * q.ld_w, k0 + k, q.d);
 #pragma unroll
                 for (int i = 0; i < NR; ++i) {
                     const float4 x = s_h[i][k >> 2];
@@ -711,9 +712,9 @@ __global__ void __launch_bounds__(256) vocab_few_rows_kernel(Work w, int n, int 
 
 // Both gradients.  A block takes 128 columns and a range of classes, its warps every eighth class: a lane keeps its four columns of h and of
 // its share of grad_h in registers, reads four values of w and writes four of grad_w per class.
-template <int NR>
-__global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(const Few q, float scale, float* __restrict__ gw, int64_t ld_gw, bool vec_gw, int chunks,
-                                                              int64_t span, Work w)
+template <int NR, bool VEC>
+__global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(const Few q, float scale, float* __restrict__ gw, int64_t ld_gw, int chunks,
+                                                                              int64_t span, Work w)
 {
     pdl_prologue();
     __shared__ float4 s_sum[8][NR][32];
@@ -725,12 +726,12 @@ __global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(co
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
         acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        h[i] = mask >> i & 1 ? few_load(q.h + i * q.ld_h, k, q.d, q.vec_h) : acc[i];
+        h[i] = mask >> i & 1 && k < q.d ? few_load<VEC>(q.h + i * q.ld_h, k, q.d) : acc[i];
     }
     if (k < q.d) {
 #pragma unroll 8
         for (int64_t v = v0 + warp; v < v1; v += 8) {
-            const float4 y = few_load(q.w + v * q.ld_w, k, q.d, q.vec_w);
+            const float4 y = few_load<VEC>(q.w + v * q.ld_w, k, q.d);
             float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < NR; i += 2) {
@@ -744,7 +745,7 @@ __global__ void __launch_bounds__(256, few_blocks(NR)) vocab_few_grads_kernel(co
             }
             float* const out = gw + v * ld_gw + k;
             o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
-            if (vec_gw && k + 4 <= q.d) {
+            if (VEC) {
                 *reinterpret_cast<float4*>(out) = o;
             } else {
                 out[0] = o.x;
@@ -1338,7 +1339,7 @@ int row_alignment(const void* p, int64_t row_bytes)
     return ptr_aligned(p, 32) && row_bytes % 32 == 0 ? 2 : 1;
 }
 
-template <int NR>
+template <int NR, bool VEC>
 int run_few(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, cudaStream_t st)
 {
     const int d = (int)v->d, k = v->k, n = (int)v->n, V = (int)v->V;
@@ -1347,16 +1348,15 @@ int run_few(const dq_vocab* v, const Targets& t, float* loss, float* lse, const 
     if (k > 0)
         ok = launch_k(vocab_targets_kernel<true>, dim3(1), dim3(256), 0, st, t.top_idx, t.top_logits, t.teacher_lse, 1.0f / t.temp, (int64_t)n, k, v->V,
                       Weights{nullptr, 0, 0, 0, 0, 1}, w) == cudaSuccess;
-    const Few q = {static_cast<const float*>(v->h), static_cast<const float*>(v->w), v->ld_h, v->ld_w, n, d, v->V, k > 0 ? w.tgt : t.labels,
-                   row_alignment(v->h, v->ld_h * 4) > 0, row_alignment(v->w, v->ld_w * 4) > 0};
-    ok = ok && launch_k(vocab_few_logits_kernel<NR>, dim3((unsigned)w.parts), dim3(256), 0, st, q, c2, loss, lse, w) == cudaSuccess;
+    const Few q = {static_cast<const float*>(v->h), static_cast<const float*>(v->w), v->ld_h, v->ld_w, n, d, v->V, k > 0 ? w.tgt : t.labels};
+    ok = ok && launch_k(vocab_few_logits_kernel<NR, VEC>, dim3((unsigned)w.parts), dim3(256), 0, st, q, c2, loss, lse, w) == cudaSuccess;
     const int parts_per_row = g ? (int)min((int64_t)32, (v->V + 1023) / 1024) : 1;
     ok = ok && launch_k(vocab_few_rows_kernel<NR>, dim3((unsigned)((g ? NR : n) * parts_per_row)), dim3(256), 0, st, w, n, V, k, parts_per_row, g != nullptr, t.labels,
                         g ? g->weight : (const float*)nullptr, t.temp, c2, 0.0f, loss, lse) == cudaSuccess;
     if (!g) return ok ? DQ_OK : DQ_ERR_CUDA;
     const float scale = g->weight ? 0.0f : t.temp;
-    ok = ok && launch_k(vocab_few_grads_kernel<NR>, dim3((unsigned)(w.chunks * w.splits)), dim3(256), 0, st, q, scale, static_cast<float*>(g->gw), g->ld_w,
-                        row_alignment(g->gw, g->ld_w * 4) > 0, w.chunks, w.span, w) == cudaSuccess;
+    ok = ok && launch_k(vocab_few_grads_kernel<NR, VEC>, dim3((unsigned)(w.chunks * w.splits)), dim3(256), 0, st, q, scale, static_cast<float*>(g->gw), g->ld_w,
+                        w.chunks, w.span, w) == cudaSuccess;
     ok = ok && launch_k(vocab_grad_h_kernel<true>, dim3((unsigned)(n * ((d + 127) / 128))), dim3(256), 0, st, w, n, d, scale, g->gh, g->ld_h) == cudaSuccess;
     return ok ? DQ_OK : DQ_ERR_CUDA;
 }
@@ -1364,7 +1364,12 @@ int run_few(const dq_vocab* v, const Targets& t, float* loss, float* lse, const 
 template <bool F32>
 int run_loss(const dq_vocab* v, const Targets& t, float* loss, float* lse, const Grads* g, const Work& w, const Device& dev, cudaStream_t st)
 {
-    if (w.few) return w.few == 2 ? run_few<2>(v, t, loss, lse, g, w, st) : run_few<8>(v, t, loss, lse, g, w, st);
+    if (w.few) {
+        const bool vec = v->d % 4 == 0 && row_alignment(v->h, v->ld_h * 4) && row_alignment(v->w, v->ld_w * 4) && (!g || row_alignment(g->gw, g->ld_w * 4));
+        auto few = w.few == 2 ? (vec ? run_few<2, true> : run_few<2, false>) : w.few == 4 ? (vec ? run_few<4, true> : run_few<4, false>)
+                                                                                         : (vec ? run_few<8, true> : run_few<8, false>);
+        return few(v, t, loss, lse, g, w, st);
+    }
     const int d = (int)v->d, k = v->k, T = w.terms, elem = F32 ? 4 : 2;
     const int64_t n = v->n, V = v->V;
     const int blocks = dev.sms * 8;
@@ -1501,7 +1506,7 @@ int64_t dq_vocab_workspace_bytes(const dq_vocab* v, int grad)
         if (bytes > most) most = bytes;
     };
     for (int64_t n = 0; n < v->n; n += 128) see(n);        // they go by n in units of 128, but for a few rows
-    see(v->n); see(2); see(kFewRows); see(kTwoTerms);
+    see(v->n); see(2); see(4); see(kFewRows); see(kTwoTerms);
     return most;
 }
 
