@@ -323,47 +323,68 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(const void* __restric
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t r0 = blockIdx.x * rows_per_block, r1 = min(n, r0 + rows_per_block);
     int before = 0;
-    for (int64_t r = threadIdx.x; r < r0; r += 256) { const int32_t t = tgt[r]; before += t >= 0 && t < V; }
-    before = __reduce_add_sync(0xFFFFFFFFu, before);
-    if (lane == 0) s_sum[warp] = before;
-    __syncthreads();
-    before = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) before += s_sum[i];
-    for (int64_t r = r0; r < r1; r += 256) {
-        __syncthreads();
-        const int64_t mine = r + threadIdx.x;
-        bool has = false;
-        if (mine < r1) { const int32_t t = tgt[mine]; has = t >= 0 && t < V; }
+    if (rows_per_block == 1 && n <= 256) {                                  // a row to a block: its target and those before it in one load
+        const bool has = (int64_t)threadIdx.x <= r0 && tgt[threadIdx.x] >= 0 && tgt[threadIdx.x] < V;
         const uint32_t bal = __ballot_sync(0xFFFFFFFFu, has);
         if (lane == 0) s_sum[warp] = __popc(bal);
+        if (threadIdx.x == r0) s_rows[0] = has;
         __syncthreads();
-        int off = 0, total = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { if (i < warp) off += s_sum[i]; total += s_sum[i]; }
-        off += __popc(bal & ((1u << lane) - 1u));
-        if (mine < r1) {
-            if (has) { w.map[before + off] = (int32_t)mine; s_rows[off] = threadIdx.x; }
-            else { s_none[threadIdx.x - off] = threadIdx.x; loss[mine] = 0.0f; if (lse) lse[mine] = 0.0f; }
-        }
-        __syncthreads();
-        if (gh) {
-            const int none = (int)min((int64_t)256, r1 - r) - total;
-            for (int i = warp; i < none; i += 8) {
-                const int64_t at = (r + s_none[i]) * ld_gh;
-                for (int j = lane; j < d; j += 32) {
-                    if (F32) static_cast<float*>(gh)[at + j] = 0.0f;
-                    else static_cast<__nv_bfloat16*>(gh)[at + j] = __float2bfloat16_rn(0.0f);
-                }
+        for (int i = 0; i < 8; ++i) before += s_sum[i];
+        if (s_rows[0]) {
+            if (threadIdx.x == 0) w.map[before - 1] = (int32_t)r0;
+            for (int j = threadIdx.x * 8; j < w.dp; j += 2048)
+                copy8<F32>(h, r0 * ld, j, d, vec, w.hp + (int64_t)(before - 1) * w.dp + j, w.n_pad * w.dp);
+        } else {
+            if (threadIdx.x == 0) { loss[r0] = 0.0f; if (lse) lse[r0] = 0.0f; }
+            for (int j = threadIdx.x; gh && j < d; j += 256) {
+                if (F32) static_cast<float*>(gh)[r0 * ld_gh + j] = 0.0f;
+                else static_cast<__nv_bfloat16*>(gh)[r0 * ld_gh + j] = __float2bfloat16_rn(0.0f);
             }
         }
-        const int per = (int)(w.dp / 8);
+    } else {
+        for (int64_t r = threadIdx.x; r < r0; r += 256) { const int32_t t = tgt[r]; before += t >= 0 && t < V; }
+        before = __reduce_add_sync(0xFFFFFFFFu, before);
+        if (lane == 0) s_sum[warp] = before;
+        __syncthreads();
+        before = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) before += s_sum[i];
+        for (int64_t r = r0; r < r1; r += 256) {
+            __syncthreads();
+            const int64_t mine = r + threadIdx.x;
+            bool has = false;
+            if (mine < r1) { const int32_t t = tgt[mine]; has = t >= 0 && t < V; }
+            const uint32_t bal = __ballot_sync(0xFFFFFFFFu, has);
+            if (lane == 0) s_sum[warp] = __popc(bal);
+            __syncthreads();
+            int off = 0, total = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { if (i < warp) off += s_sum[i]; total += s_sum[i]; }
+            off += __popc(bal & ((1u << lane) - 1u));
+            if (mine < r1) {
+                if (has) { w.map[before + off] = (int32_t)mine; s_rows[off] = threadIdx.x; }
+                else { s_none[threadIdx.x - off] = threadIdx.x; loss[mine] = 0.0f; if (lse) lse[mine] = 0.0f; }
+            }
+            __syncthreads();
+            if (gh) {
+                const int none = (int)min((int64_t)256, r1 - r) - total;
+                for (int i = warp; i < none; i += 8) {
+                    const int64_t at = (r + s_none[i]) * ld_gh;
+                    for (int j = lane; j < d; j += 32) {
+                        if (F32) static_cast<float*>(gh)[at + j] = 0.0f;
+                        else static_cast<__nv_bfloat16*>(gh)[at + j] = __float2bfloat16_rn(0.0f);
+                    }
+                }
+            }
+            const int per = (int)(w.dp / 8);
 #pragma unroll 4
-        for (int t = threadIdx.x; t < total * per; t += 256) {
-            const int i = t / per, j = (t - i * per) * 8;
-            copy8<F32>(h, (r + s_rows[i]) * ld, j, d, vec, w.hp + (int64_t)(before + i) * w.dp + j, w.n_pad * w.dp);
+            for (int t = threadIdx.x; t < total * per; t += 256) {
+                const int i = t / per, j = (t - i * per) * 8;
+                copy8<F32>(h, (r + s_rows[i]) * ld, j, d, vec, w.hp + (int64_t)(before + i) * w.dp + j, w.n_pad * w.dp);
+            }
+            before += total;
         }
-        before += total;
     }
     if (blockIdx.x == q.first - 1) {
         if (threadIdx.x == 0) { w.ctrl->count = before; w.ctrl->status = DQ_OK; }
