@@ -1,15 +1,17 @@
 """The vocabulary losses on the GPU against their definitions in 64 bits.
 
 Tolerances, elementwise, from the arithmetic (u = 2^-24, the rounding of fp32):
-  logits    products of bf16 values (or of fp32 values as three bf16 terms) are exact; a sum runs over segments of 512 in the
-            tensor cores, which cut off toward zero at each of 32 steps (and align the 16 products of a step): at most
-            2 * 32 * 2u of A = sum |h_i w_i|, six times as many steps for the fp32 terms, plus one rounding per segment.
+  logits    products of bf16 values (or of fp32 values as three bf16 terms) are exact; a sum runs over segments in the tensor
+            cores, which cut off toward zero at each step of 16 (and align the 16 products of a step): at most 2 * 2u of
+            A = sum |h_i w_i| a step, 64 steps a segment (fp32: 32, and six times as many steps in all), plus one rounding per
+            segment.  What is given back for the cut-off, at most 18u of the logit, has the other sign and is smaller.
   lse       moves by no more than the largest logit error; exp2 is good to 4u, the sum of up to V terms of one sign adds
             no more than 8u in total along any tree used here (128 terms as four chains of 32, then pairs), log and the
             final rounding 2u |lse|.
   gradient  g = weight T (S p - q) has the relative error of p: the logit error of the label's row / T twice (z and lse),
             plus 2^-8 relative where it is rounded to bf16 (3 terms for fp32: 2^-24).  A product adds the segment error
-            above, relative to |g| |w|, and the output's rounding: half a step of its type.
+            above with up to 256 steps a segment for bf16, as do the logits of the gradient's own pass, relative to
+            |g| |w|, and the output's rounding: half a step of its type.
 """
 import math
 
@@ -35,11 +37,12 @@ def _torch():
     return torch
 
 
-def _sum_err(K, f32):
-    """Relative to the sum of magnitudes: tensor-core segments, then one rounding per segment."""
+def _sum_err(K, f32, segment=64):
+    """Relative to the sum of magnitudes: tensor-core segments of so many steps, then one rounding per segment."""
     pairs = 6 if f32 else 1
+    segment = 32 if f32 else segment
     steps = -(-K // 64) * 4 * pairs
-    return 2 * 2 * U * min(32, steps) + U * -(-steps // 32) + (4 * U if f32 else 0)
+    return 2 * 2 * U * min(segment, steps) + U * -(-steps // segment) + (4 * U if f32 else 0)
 
 
 class Ref:
@@ -67,6 +70,7 @@ class Ref:
         p = torch.exp(z - self.lse[:, None])
         g = (mass[:, None] * p).scatter_add_(1, at, -q) * self.wt[:, None]
         # |g| error: of p and q each by relative error, and the rounding
+        zerr = zerr + (H.abs() @ W.abs().t() / T).max(1).values * (_sum_err(d, f32, 256) - _sum_err(d, f32))
         pe = (mass[:, None] * p) * (2 * zerr + 24 * U + 4 * U * self.lse.abs())[:, None] + 2.0 ** -125        # exp2 flushes below 2^-126
         qe = torch.zeros_like(p).scatter_add_(1, at, q * (8 * U * (1 + logq.abs())))
         ge = (pe + qe) * self.wt.abs()[:, None] + g.abs() * (2 * U if f32 else 2.0 ** -8 * 1.01)
@@ -74,8 +78,8 @@ class Ref:
         half = U if f32 else 2.0 ** -8
         self.gh, self.gw = g @ W, g.t() @ H
         tiny = 2.0 ** -133 if not f32 else 2.0 ** -149                    # half a step of the smallest values
-        self.gh_err = 1.01 * (ge @ W.abs() + (g.abs() @ W.abs()) * (_sum_err(w.shape[0], f32) + 8 * U) + gm @ W.abs() * 2 * U) + self.gh.abs() * half * 1.01 + tiny
-        self.gw_err = 1.01 * (ge.t() @ H.abs() + (g.abs().t() @ H.abs()) * (_sum_err(n, f32) + 8 * U) + gm.t() @ H.abs() * 2 * U) + self.gw.abs() * half * 1.01 + tiny
+        self.gh_err = 1.01 * (ge @ W.abs() + (g.abs() @ W.abs()) * (_sum_err(w.shape[0], f32, 256) + 8 * U) + gm @ W.abs() * 2 * U) + self.gh.abs() * half * 1.01 + tiny
+        self.gw_err = 1.01 * (ge.t() @ H.abs() + (g.abs().t() @ H.abs()) * (_sum_err(n, f32, 256) + 8 * U) + gm.t() @ H.abs() * 2 * U) + self.gw.abs() * half * 1.01 + tiny
 
     def check(self, loss=None, lse=None, gh=None, gw=None, where=""):
         torch = _torch()
