@@ -85,7 +85,7 @@ struct Work {
     int64_t bytes;
 };
 
-constexpr int kTwoTerms = 16;                             // rows up to which g of bf16 calls has two terms
+constexpr int kTwoTerms = 32;                             // rows up to which g of bf16 calls has two terms
 constexpr int kFewRows = 8;                               // see vocab_few_logits_kernel
 __host__ __device__ constexpr int few_blocks(int rows) { return rows < 8 ? 3 : 2; }      // of vocab_few_grads_kernel on an SM
 

@@ -539,10 +539,10 @@ def test_workspace_is_enough_for_fewer_rows(dq):
         for d, V in ((64, 1000), (1536, 9791), (24, 70001)):
             w = torch.zeros(V, d, dtype=dt, device="cuda")
             for grad in (False, True):
-                for n in (1, 2, 8, 9, 16, 17, 100, 128, 129, 256, 257, 700):
+                for n in (1, 2, 8, 9, 16, 17, 32, 33, 100, 128, 129, 256, 257, 700):
                     h = torch.zeros(n, d, dtype=dt, device="cuda")
                     most = dq.Vocab.workspace_bytes(h, w, grad=grad)
-                    for m in (1, 2, 3, 8, 9, 16, 17, 64, 128, 129, 250, 256, 384, 385, 512, 640):
+                    for m in (1, 2, 3, 8, 9, 16, 17, 32, 33, 64, 128, 129, 250, 256, 384, 385, 512, 640):
                         if m <= n:
                             assert dq.Vocab.workspace_bytes(h[:m], w, grad=grad) <= most, (dt, d, V, grad, n, m)
 
